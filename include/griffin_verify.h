@@ -420,6 +420,107 @@ int griffin_draft_tree(griffin_draft *draft, int32_t batch, const int32_t *prefi
                        const float *root_features, int32_t k, int32_t depth, int32_t n_total,
                        int32_t *n_nodes_out, int32_t *tokens_out, int32_t *parents_out, float *scores_out);
 
+/* ------------------------------------------------------- 8-bit paged cache
+ * A KV cache in pages of page_slots token slots (a multiple of 32), in 8 bits.
+ * Slot s of sequence b is slot s % page_slots of page table[b][s / page_slots];
+ * pages may be shared by sequences that only read them.  A tile is 32 slots of
+ * one page and KV head; it holds e4m3 numbers (4 significant bits, up to 448)
+ * and one exponent for its keys and one for its values: a stored x stands for
+ * x * 2^exponent.  One layer's pool, device memory of the caller, k and v
+ * 16-byte aligned:
+ *   k      e4m3 [n_pages][n_kv_heads][page_slots / 32][head_dim / 16][32][16]
+ *          (16 dimensions of a slot together; keys after rotation)
+ *   v      e4m3 [n_pages][n_kv_heads][page_slots / 32][head_dim][32]
+ *   k_exp, v_exp  int8 [n_pages][n_kv_heads][page_slots / 32]
+ * head_dim 64 or 128; n_pages * n_kv_heads * page_slots / 32 below 2^31.
+ *
+ * Both calls take their sequences' state (table, lengths, counts, path, anc)
+ * from device memory, allocate nothing, copy nothing and wait for nothing, so
+ * they can be captured and replayed with that state changed in place.  The
+ * host cannot check it, the kernels do: a page outside [0, n_pages), a length
+ * or count out of range or a source row out of range sets a bit of *status (if
+ * given; device int32, or-ed, never cleared here) and never leads to an access
+ * outside of the pool. */
+typedef struct griffin_pool {
+  void *k, *v, *k_exp, *v_exp;
+  int32_t n_pages, page_slots, n_kv_heads, head_dim;
+} griffin_pool;
+
+#define GRIFFIN_PAGED_BAD_PAGE 1
+#define GRIFFIN_PAGED_BAD_LENGTH 2
+#define GRIFFIN_PAGED_BAD_ROW 4
+
+#define GRIFFIN_BF16 0
+#define GRIFFIN_FP16 1
+#define GRIFFIN_FP32 2
+
+/* Device rows [batch][rows][heads][head_dim]: strides in elements (>= 0), the
+ * last dimension contiguous, aligned to an element at least. */
+typedef struct griffin_rows {
+  const void *data;
+  int64_t stride_seq, stride_row, stride_head;
+} griffin_rows;
+
+typedef struct griffin_append {
+  griffin_pool pool;
+  const int32_t *table;   /* [batch][table_stride], table_cols of them used */
+  const int32_t *lengths; /* [batch] cached slots before the call */
+  const int32_t *counts;  /* [batch] new rows, 0 .. max_new; NULL: max_new each */
+  const int32_t *path;    /* [batch][path_stride] source row of each new one; NULL: row j */
+  int32_t *status;        /* optional */
+  griffin_rows k, v;      /* [batch][rows][n_kv_heads] */
+  double rope_base;       /* rotate the keys by their slot's angle; 0: they are rotated already */
+  int32_t table_stride, table_cols, path_stride, batch, rows, max_new, dtype;
+} griffin_append;
+
+/* Append rows to the cache: sequence b's new row j goes to slot lengths[b] + j.
+ * Keys are rotated on the way (rotate-half, angle slot * rope_base^(-2i/dh)).
+ * A tile's exponent becomes the smallest e with |x| <= 448 * 2^e for its new
+ * finite values (-110 at least), and stays at least what its earlier slots
+ * have; where it rises those are rounded again.  Numbers are rounded once, to
+ * nearest even; an infinity becomes the largest number, a NaN stays one.
+ * Later slots keep their bytes.  lengths is not changed.  A sequence whose
+ * length or count is out of range, rows whose source is, and tiles whose page
+ * is, are left out (and told in *status).  No two sequences of a call may
+ * append to one page.  Errors: EINVAL, ESHAPE, EHIP. */
+int griffin_paged_append(const griffin_append *args, void *hip_stream);
+
+typedef struct griffin_attention {
+  griffin_pool pool;
+  const int32_t *table;   /* [batch][table_stride], table_cols of them used */
+  const int32_t *lengths; /* [batch] cached slots */
+  const int32_t *counts;  /* [batch] nodes, 0 .. nodes; NULL: nodes each */
+  const uint64_t *anc;    /* [batch][nodes] bits of the nodes that a node sees (griffin_tree_prepare); NULL: a chain */
+  int32_t *status;        /* optional */
+  griffin_rows q;         /* [batch][nodes][n_q_heads], rotated */
+  griffin_rows k, v;      /* [batch][nodes][n_kv_heads] the nodes' own, not cached yet; k rotated */
+  griffin_rows out;       /* [batch][nodes][n_q_heads] */
+  float scale;            /* of the scores, > 0 (1 / sqrt(head_dim)) */
+  int32_t table_stride, table_cols, max_length, batch, nodes, n_q_heads, dtype, window, sinks;
+} griffin_attention;
+
+/* Attention of up to 64 nodes per sequence (a single token, a chain, a tree):
+ * node i sees the cached slots and the nodes of anc[i].  It stands at position
+ * lengths[b] + (bits of anc[i] other than i); the r-th node it sees stands at
+ * position lengths[b] + r.  With window > 0 it sees what stands less than
+ * window positions before it, or at one of the first `sinks` positions; pages
+ * that no node sees are not read and need not exist.  A node that sees nothing
+ * gets zeros, and rows of absent nodes are left as they were.  What a masked
+ * place holds, NaN included, reaches no row.
+ *   max_length: no length is larger (it bounds the launch); -1: the table's
+ *               capacity.
+ * Scores, probabilities' sums and outputs are fp32; fp32 inputs enter the
+ * matrix cores as two fp16 parts, others' probabilities as one.  The rows of a
+ * sequence with an invalid page or length become NaN.  Head h reads KV head
+ * h / (n_q_heads / n_kv_heads).  The workspace (16-byte aligned, of
+ * griffin_paged_attention_workspace bytes; 0 for arguments that the call
+ * refuses) belongs to the call until its work is done.  The same call gives the same
+ * bits; the other sequences' lengths can change a sequence's last bits.
+ * Errors: EINVAL, ESHAPE, ETREE (nodes), ECAPACITY (max_length beyond the
+ * table), ENOMEM (workspace_bytes), EHIP. */
+size_t griffin_paged_attention_workspace(const griffin_attention *args);
+int griffin_paged_attention(const griffin_attention *args, void *workspace, size_t workspace_bytes, void *hip_stream);
+
 /* Kernel classes of one verification pass, for griffin_profile_*. */
 #define GRIFFIN_KC_QKV 0     /* QKV projection GEMM */
 #define GRIFFIN_KC_ROPE 1    /* rotary embedding + tree K/V write */

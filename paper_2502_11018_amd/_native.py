@@ -96,6 +96,9 @@ def _load() -> ctypes.CDLL:
         "griffin_draft_extend": (c_int32, [c_void_p, c_int32, I32P, I32P, I32P, c_void_p]),
         "griffin_draft_tree": (c_int32, [c_void_p, c_int32, I32P, I32P, c_void_p, c_int32, c_int32, c_int32, I32P,
                                          I32P, I32P, F32P]),
+        "griffin_paged_append": (c_int32, [c_char_p, c_void_p]),
+        "griffin_paged_attention_workspace": (c_size_t, [c_char_p]),
+        "griffin_paged_attention": (c_int32, [c_char_p, c_void_p, c_size_t, c_void_p]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -112,6 +115,7 @@ EXPORTED = ("griffin_kv_cache_bytes", "griffin_verify_init", "griffin_verify_ste
             "griffin_draft_init", "griffin_draft_free", "griffin_draft_context", "griffin_draft_step",
             "griffin_draft_tree", "griffin_read_features", "griffin_draft_extend",
             "griffin_set_activation_precision", "griffin_read_router_logits", "griffin_read_margins",
-            "griffin_accept_sampled_walk_noalloc")
+            "griffin_accept_sampled_walk_noalloc", "griffin_paged_append", "griffin_paged_attention",
+            "griffin_paged_attention_workspace")
 KERNEL_CLASSES = ("qkv_gemm", "rope_kv_write", "tree_attention", "o_gemm", "residual_rmsnorm", "gate_up_gemm",
                   "down_gemm", "lm_head_gemm", "argmax_accept_route", "attn_merge")

@@ -1,0 +1,217 @@
+// Appending keys and values to the 8-bit paged cache (paged.h).
+//
+// New row j of sequence b goes to slot s = length_b + j.  Its key is rotated
+// by the angle of position s on the way (k_i cos - k_{i+dh/2} sin, k_{i+dh/2}
+// cos + k_i sin; the angle in fp64, reduced to a fraction of a turn there, its
+// sine and cosine in fp32).  A tile's exponent is the smallest e with |x| <=
+// 448 * 2^e for all its new finite values, and not below the one that its
+// earlier slots have; where it rises those are rounded again.  The numbers are
+// rounded to e4m3 once, to nearest even, from fp32; an infinity becomes the
+// largest number, a NaN stays one.
+//
+// A workgroup owns a tile (every slot of it that this call writes or rounds
+// again) for some heads, one after the other, so that no two workgroups write
+// one tile and the 32 * dh / 2 sines are computed once for all its heads.
+// Later slots of the tile keep their bytes.
+
+#include <algorithm>
+
+#include "paged.h"
+
+namespace griffin {
+
+namespace {
+
+// Smallest e with amax <= 448 * 2^e (448 = 1.75 * 2^8), at least PAGED_E_MIN.
+__device__ __forceinline__ int exponent_for(float amax) {
+  const uint32_t u = __float_as_uint(amax);
+  const int e = (int)(u >> 23) - 127 - 8 + ((u & 0x7fffff) > 0x600000 ? 1 : 0);
+  return max(e, PAGED_E_MIN);  // subnormal and zero: far below
+}
+
+__device__ __forceinline__ float finite_abs(float x) {
+  const float a = fabsf(x);
+  return a <= 3.402823466e38f ? a : 0.f;
+}
+
+// 4 values to e4m3, the first in the low byte
+__device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d) {
+  // the conversion turns what is above 448 into a NaN: clamp, which a NaN passes
+  auto sat = [](float x) { return x > 448.f ? 448.f : x < -448.f ? -448.f : x; };
+  const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(sat(a), sat(b), 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(sat(c), sat(d), lo, true);
+}
+
+__device__ __forceinline__ uint32_t rescale_e4m3(uint32_t w, float f) {
+  return pack_e4m3(__builtin_amdgcn_cvt_f32_fp8(w, 0) * f, __builtin_amdgcn_cvt_f32_fp8(w, 1) * f,
+                   __builtin_amdgcn_cvt_f32_fp8(w, 2) * f, __builtin_amdgcn_cvt_f32_fp8(w, 3) * f);
+}
+
+// Threads: DH * 2, (slot, j) = (t % 32, t / 32): the key's dims 8 j .. and
+// DH / 2 + 8 j .. of a slot, and of the values 4 slots x 4 dims.
+template <int DH>
+__global__ __launch_bounds__(DH * 2) void paged_append_kernel(PagedAppend a) {
+  constexpr int NT = DH * 2, NW = NT / 64, HALF = DH / 2;
+  __shared__ float red[2][2][NW];
+  const int t = threadIdx.x;
+  const int groups = (a.pool.Hkv + a.heads_per_wg - 1) / a.heads_per_wg;
+  const int tiles_max = (a.max_new + 31) / 32 + 1;
+  int id = blockIdx.x;
+  const int g = id % groups;
+  id /= groups;
+  const int tl = id % tiles_max;
+  id /= tiles_max;
+  const int b = id % a.batch, layer = id / a.batch;
+
+  const int len = a.tab.lengths[b];
+  int n = a.counts ? a.counts[(long long)b * a.counts_stride] + a.counts_add : a.max_new;
+  const bool odd = len < 0 || n < 0 || n > a.max_new || (long long)len + n > a.tab.most;
+  if (odd) {  // nothing of such a sequence is written
+    if (a.status && t == 0) atomicOr(a.status, PAGED_BAD_LENGTH);
+    return;
+  }
+  const int tile = len / 32 + tl;
+  const int s0 = tile * 32;
+  if (n == 0 || s0 >= len + n) return;
+  const int page = a.tab.pages[(long long)b * a.tab.stride + tile / a.pool.tpp];
+  if (page < 0 || page >= a.pool.n_pages) {
+    if (a.status && t == 0) atomicOr(a.status, PAGED_BAD_PAGE);
+    return;
+  }
+  const int h0 = g * a.heads_per_wg, h1 = min(h0 + a.heads_per_wg, a.pool.Hkv);
+  const long long tile0 = layer * a.pool_layer + (long long)page * a.pool.Hkv * a.pool.tpp + tile % a.pool.tpp;
+
+  // source row of a slot: -1 none (an earlier or a later slot), -2 out of range
+  auto row_of = [&](int slot) -> int {
+    const int j = slot - len;
+    if (j < 0 || j >= n) return -1;
+    if (!a.path) return j;
+    if (a.path_first && j == 0) return 0;
+    const int r = a.path[(long long)b * a.path_stride + j - a.path_first];
+    return r >= 0 && r < a.rows ? r : -2;
+  };
+  const int slot = s0 + t % 32, j = t / 32;
+  const int krow = row_of(slot);
+  // values: slots 4 vg .. + 3, dims 4 vd .. + 3
+  const int vg = t % 8, vd = t / 8;
+  int vrow[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) vrow[i] = row_of(s0 + 4 * vg + i);
+  if (a.status && krow == -2) atomicOr(a.status, PAGED_BAD_ROW);
+  const bool held = s0 < len;  // the tile has earlier slots
+
+  float cs[8], sn[8];
+  if (a.rotate) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      double rev = slot * a.inv_rev[8 * j + i];
+      rev -= rint(rev);
+      sincospif(2.f * (float)rev, &sn[i], &cs[i]);
+    }
+  }
+  const long long kb = layer * a.rows_layer + b * a.k.sb, vb = layer * a.rows_layer + b * a.v.sb;
+  for (int h = h0; h < h1; ++h) {
+    float x[8], y[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = y[i] = 0.f;
+    if (krow >= 0) {
+      const long long at = kb + krow * a.k.sr + h * a.k.sh + 8 * j;
+      load8(a.k.p, at, a.dtype, a.k.vec, x);
+      load8(a.k.p, at + HALF, a.dtype, a.k.vec, y);
+    }
+    float4 z[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      z[i] = vrow[i] >= 0 ? load4(a.v.p, vb + vrow[i] * a.v.sr + h * a.v.sh + 4 * vd, a.dtype, a.v.vec)
+                          : make_float4(0.f, 0.f, 0.f, 0.f);
+    const long long ti = tile0 + (long long)h * a.pool.tpp;
+    int ke = PAGED_E_MIN, ve = PAGED_E_MIN;
+    if (held) ke = a.pool.ke[ti], ve = a.pool.ve[ti];
+    if (a.rotate) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float u = x[i], w = y[i];
+        x[i] = u * cs[i] - w * sn[i];
+        y[i] = w * cs[i] + u * sn[i];
+      }
+    }
+    float mk = 0.f, mv = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) mk = fmaxf(mk, fmaxf(finite_abs(x[i]), finite_abs(y[i])));
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      mv = fmaxf(mv, fmaxf(fmaxf(finite_abs(z[i].x), finite_abs(z[i].y)), fmaxf(finite_abs(z[i].z), finite_abs(z[i].w))));
+    mk = wave_max(mk), mv = wave_max(mv);
+    float(&rd)[2][NW] = red[h & 1];  // two sets: the next head's maxima do not meet this one's readers
+    if ((t & 63) == 0) rd[0][t >> 6] = mk, rd[1][t >> 6] = mv;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < NW; ++i) mk = fmaxf(mk, rd[0][i]), mv = fmaxf(mv, rd[1][i]);
+    const int ken = max(ke, exponent_for(mk)), ven = max(ve, exponent_for(mv));
+    uint8_t* kt = a.pool.k + ti * 32 * DH;
+    uint8_t* vt = a.pool.v + ti * 32 * DH;
+    // keys: [DH / 16][32][16]
+    const int c = j / 2, o = 8 * (j % 2);
+    uint2* k0 = reinterpret_cast<uint2*>(kt + (c * 32 + t % 32) * 16 + o);
+    uint2* k1 = reinterpret_cast<uint2*>(kt + ((c + DH / 32) * 32 + t % 32) * 16 + o);
+    if (krow >= 0) {
+      const float f = pow2i(-ken);
+      *k0 = make_uint2(pack_e4m3(x[0] * f, x[1] * f, x[2] * f, x[3] * f), pack_e4m3(x[4] * f, x[5] * f, x[6] * f, x[7] * f));
+      *k1 = make_uint2(pack_e4m3(y[0] * f, y[1] * f, y[2] * f, y[3] * f), pack_e4m3(y[4] * f, y[5] * f, y[6] * f, y[7] * f));
+    } else if (slot < len && ken > ke) {
+      const float f = pow2i(ke - ken);
+      const uint2 p = *k0, q = *k1;
+      *k0 = make_uint2(rescale_e4m3(p.x, f), rescale_e4m3(p.y, f));
+      *k1 = make_uint2(rescale_e4m3(q.x, f), rescale_e4m3(q.y, f));
+    }
+    // values: [DH][32], a word of 4 slots for each of 4 dims
+    {
+      const float f = pow2i(-ven), g2 = pow2i(ve - ven);
+      uint32_t keep = 0;  // bytes that stay
+      bool any_new = false, any_old = false;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (vrow[i] < 0) keep |= 0xffu << (8 * i);
+        any_new |= vrow[i] >= 0;
+        any_old |= s0 + 4 * vg + i < len;
+      }
+      if (any_new || (any_old && ven > ve)) {
+        uint32_t older = 0;  // bytes of earlier slots
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (s0 + 4 * vg + i < len) older |= 0xffu << (8 * i);
+        const float* zf = &z[0].x;
+#pragma unroll
+        for (int d = 0; d < 4; ++d) {
+          uint32_t* w = reinterpret_cast<uint32_t*>(vt + (4 * vd + d) * 32 + 4 * vg);
+          auto at = [&](int i) { return d == 0 ? z[i].x : d == 1 ? z[i].y : d == 2 ? z[i].z : z[i].w; };
+          uint32_t u = pack_e4m3(at(0) * f, at(1) * f, at(2) * f, at(3) * f);
+          if (keep) {
+            uint32_t was = *w;
+            if (older && ven > ve) was = (was & ~older) | (rescale_e4m3(was, g2) & older);
+            u = (u & ~keep) | (was & keep);
+          }
+          *w = u;
+        }
+      }
+    }
+    if (t == 0) a.pool.ke[ti] = (int8_t)ken, a.pool.ve[ti] = (int8_t)ven;
+  }
+}
+
+}  // namespace
+
+hipError_t launch_paged_append(PagedAppend a, hipStream_t s) {
+  const long long tiles = (long long)a.layers * a.batch * ((a.max_new + 31) / 32 + 1);
+  // One head per workgroup until there are enough of them, then all heads of a
+  // tile, which share the tile's sines.
+  a.heads_per_wg = (int)std::min<long long>(a.pool.Hkv, std::max<long long>(1, tiles * a.pool.Hkv / 1024));
+  const long long grid = tiles * ((a.pool.Hkv + a.heads_per_wg - 1) / a.heads_per_wg);
+  if (grid > 0x7fffffffLL) return hipErrorInvalidValue;
+  if (a.pool.dh == 128) hipLaunchKernelGGL(paged_append_kernel<128>, dim3((unsigned)grid), dim3(256), 0, s, a);
+  else if (a.pool.dh == 64) hipLaunchKernelGGL(paged_append_kernel<64>, dim3((unsigned)grid), dim3(128), 0, s, a);
+  else return hipErrorInvalidValue;
+  return hipGetLastError();
+}
+
+}  // namespace griffin
