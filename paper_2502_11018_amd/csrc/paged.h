@@ -93,18 +93,32 @@ struct PagedAttn {
   int units;              // upper bound of the units (grid)
   float* part_o;          // [units][Hkv][G * nodes][dh]
   float* part_ml;         // [units][Hkv][G * nodes][2]
+  int2* first_unit;       // [batch] first unit and units of a sequence that has any
+  int wide;               // waves of a workgroup of the wide kernel, 0: the other one (paged_plan)
   int32_t* status;
 };
 hipError_t launch_paged_attention(const PagedAttn& a, hipStream_t s);
 
-// Shape of the call, from host values alone: fills a.cut and a.units.
-void paged_plan(PagedAttn& a, int max_length);
-size_t paged_workspace_floats(const PagedAttn& a);
+// Shape of the call, from host values alone: fills a.cut, a.units and the
+// workgroup's shape.  Not 0: too many tiles.
+int paged_plan(PagedAttn& a, int max_length);
+// Lays the call's workspace out at `base` and returns its bytes.
+size_t paged_workspace(PagedAttn& a, void* base);
 
 // ------------------------------------------------------------- device helpers
 
 __device__ __forceinline__ float pow2i(int e) {  // 2^e, e clamped to the normal range
   return __uint_as_float((uint32_t)(min(max(e, -126), 127) + 127) << 23);
+}
+
+// 8 consecutive 16-bit values
+__device__ __forceinline__ u32x4 load8_raw(const void* p, long long at, int vec) {
+  const uint16_t* h = static_cast<const uint16_t*>(p) + at;
+  if (vec) return ld_u4(h);
+  u32x4 w;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = h[2 * i] | (uint32_t)h[2 * i + 1] << 16;
+  return w;
 }
 
 // 8 consecutive values as fp32
@@ -120,14 +134,7 @@ __device__ __forceinline__ void load8(const void* p, long long at, int dtype, in
     }
     return;
   }
-  const uint16_t* h = static_cast<const uint16_t*>(p) + at;
-  u32x4 w;
-  if (vec) {
-    w = ld_u4(h);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = h[2 * i] | (uint32_t)h[2 * i + 1] << 16;
-  }
+  const u32x4 w = load8_raw(p, at, vec);
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const uint16_t u = w[i / 2] >> (16 * (i & 1));

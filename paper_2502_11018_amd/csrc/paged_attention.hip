@@ -41,6 +41,11 @@ namespace {
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+struct KeyPair {
+  u32x4 a, b;
+};
+__device__ __forceinline__ f16x8 as_f16x8(const u32x4& v) { return __builtin_bit_cast(f16x8, v); }
 
 // The cached tiles that some node of a sequence of `len` slots sees: the first
 // `sink` ones, then those from `lo` on; n in all.
@@ -63,73 +68,54 @@ __device__ __forceinline__ int checked_len(const PagedTable& t, int b, bool* bad
   return ok ? len : 0;
 }
 
-// Tiles per unit: the same for every workgroup of both kernels (whole waves
-// call these).
-__device__ int tiles_per_unit(const PagedAttn& a) {
-  const int lane = threadIdx.x & 63;
-  long long total = 0;
-  for (int b0 = 0; b0 < a.batch; b0 += 64) {
-    bool bad = false;
-    const int b = b0 + lane;
-    int n = b < a.batch ? seq_tiles(checked_len(a.tab, b, &bad), a.cut).n : 0;
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o, 64);
-    total += n;
-  }
-  const long long per = (total + a.cut.target - 1) / a.cut.target;
-  return (int)max((long long)a.cut.least, per);
+// Sum over the lanes that hold sequences (uniform; whole waves call these).
+__device__ __forceinline__ int lanes_sum(int n, int batch) {
+  for (int o = 1; o < 64 && o < batch; o <<= 1) n += __shfl_xor(n, o, 64);
+  return __builtin_amdgcn_readfirstlane(n);
 }
 
-// First unit of sequence `b` and the sequence's units.
-struct Units {
-  int first, n;
-};
-__device__ Units units_of(const PagedAttn& a, int per, int b) {
-  const int lane = threadIdx.x & 63;
-  int first = 0;
-  for (int b0 = 0;; b0 += 64) {
-    bool bad = false;
-    const int x = b0 + lane;
-    const int n = x < a.batch ? (seq_tiles(checked_len(a.tab, x, &bad), a.cut).n + per - 1) / per : 0;
-    int before = x < b ? n : 0;
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) before += __shfl_xor(before, o, 64);
-    first += before;
-    if (b < b0 + 64) return {first, __shfl(n, b - b0, 64)};
-  }
-}
-// The sequence of unit u: {sequence (-1: none), split, splits}.
+// The sequence of unit u: {sequence (-1: none), split, splits}.  A unit holds
+// at most max(least, ceil(all tiles / target)) tiles, and a sequence's units
+// the same number each to one.
 struct UnitAt {
   int b, split, n;
 };
-__device__ UnitAt unit_at(const PagedAttn& a, int per, int u) {
+__device__ UnitAt unit_at(const PagedAttn& a, int u) {
   const int lane = threadIdx.x & 63;
+  bool bad = false;
+  auto tiles = [&](int b) { return b < a.batch ? seq_tiles(checked_len(a.tab, b, &bad), a.cut).n : 0; };
+  const int own = tiles(lane);
+  uint32_t total = lanes_sum(own, a.batch);
+  for (int b0 = 64; b0 < a.batch; b0 += 64) total += lanes_sum(tiles(b0 + lane), 64);
+  const int per = max((uint32_t)a.cut.least, (total + a.cut.target - 1) / a.cut.target);
   int first = 0;
   for (int b0 = 0; b0 < a.batch; b0 += 64) {
-    bool bad = false;
-    const int x = b0 + lane;
-    const int n = x < a.batch ? (seq_tiles(checked_len(a.tab, x, &bad), a.cut).n + per - 1) / per : 0;
-    int end = n;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
+    const int n = ((b0 ? tiles(b0 + lane) : own) + per - 1) / per;
+    int end = n;  // inclusive sum over the lanes
+    for (int o = 1; o < 64 && o < a.batch; o <<= 1) {
       const int y = __shfl_up(end, o, 64);
       if (lane >= o) end += y;
     }
     const unsigned long long in = __ballot(u >= first + end - n && u < first + end);
     if (in) {
       const int l = __builtin_ctzll(in);
-      return {b0 + l, u - first - __shfl(end - n, l, 64), __shfl(n, l, 64)};
+      return {b0 + l, u - first - __builtin_amdgcn_readlane(end - n, l), __builtin_amdgcn_readlane(n, l)};
     }
-    first += __shfl(end, 63, 64);
+    first += __builtin_amdgcn_readlane(end, 63);
   }
   return {-1, 0, 0};
 }
 
-// 8 e4m3 of two words as fp16, times 2^e of the factor `s`
+// 8 e4m3 of two words as fp16 or bf16 (both exact), times 2^e of the factor `s`
 __device__ __forceinline__ f16x8 cvt8(uint32_t a, uint32_t b, float s) {
   const f16x2 p = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, s, false), q = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, s, true);
   const f16x2 r = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, s, false), t = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, s, true);
   return f16x8{p.x, p.y, q.x, q.y, r.x, r.y, t.x, t.y};
+}
+__device__ __forceinline__ bf16x8 cvt8_bf16(uint32_t a, uint32_t b) {
+  const bf16x2 p = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.f, false), q = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.f, true);
+  const bf16x2 r = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.f, false), t = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.f, true);
+  return bf16x8{p.x, p.y, q.x, q.y, r.x, r.y, t.x, t.y};
 }
 
 // nodes that node i sees, and its position behind the cached slots
@@ -140,279 +126,464 @@ __device__ __forceinline__ int depth_of(uint64_t anc, int i) { return __builtin_
 
 constexpr float NO_MAX = -3e38f;  // reference of a row that has seen no key
 
-template <int DH, bool SPLIT>
-__global__ __launch_bounds__(256, 2) void paged_attention_kernel(PagedAttn a) {
-  constexpr int NW = 4;
-  constexpr int KP = DH / 32;  // 1 KB pieces of a tile's keys, two MFMAs each
-  constexpr int DB = DH / 32;  // 1 KB pieces of its values: 32 dims each
-  __shared__ float so[NW][32 * DH];
-  __shared__ float sm[NW][32], sl[NW][32];
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int col = lane & 31, hh = lane >> 5;
-  const int G = a.Hq / a.pool.Hkv, R = G * a.nodes, rtiles = (R + 31) / 32;
+// How q enters the matrix cores, by its type and the kernel:
+//   Q_BF16   bf16 as it is, keys converted to bf16
+//   Q_FP8    bf16 as two e4m3 parts (4 + 4 bits, exact down to 2^-21 of the row's largest value), keys
+//            not converted at all: for waves with many tiles, as splitting q costs what converting
+//            the keys of a dozen tiles does
+//   Q_F16    fp16 as it is
+//   Q_SPLIT  fp32 (or bf16 hi + lo) as two fp16 parts
+enum QueryForm : int { Q_BF16, Q_FP8, Q_F16, Q_SPLIT };
 
-  // XCD-aware decode: workgroups go round-robin over the 8 XCDs, so the row
-  // tiles of one (unit, KV head) get the same id % 8 and share its L2
-  const int id = blockIdx.x, rest = id >> 3;
-  const int rt = rest % rtiles;
-  const int st = (rest / rtiles) * 8 + (id & 7);
-  const int hk = st % a.pool.Hkv, u = st / a.pool.Hkv;
-  const int per = tiles_per_unit(a);
-  const UnitAt at = unit_at(a, per, u);
-  if (at.b < 0) return;  // uniform
-  const int b = at.b;
-  bool bad = false;
-  const int len = checked_len(a.tab, b, &bad);
-  const SeqTiles seq = seq_tiles(len, a.cut);
-  const int i0 = (int)((long long)seq.n * at.split / at.n), i1 = (int)((long long)seq.n * (at.split + 1) / at.n);
-  const int count = a.counts ? a.counts[b] : a.nodes;
+constexpr bool probs_split(int qf) { return qf == Q_F16 || qf == Q_SPLIT; }  // probabilities as two fp16 parts
 
-  // row of this lane
-  const int row = rt * 32 + col, rowc = min(row, R - 1);
-  const int node = rowc % a.nodes, hq = hk * G + rowc / a.nodes;
-  int pos = 0;
-  if (a.cut.window) pos = len + depth_of(anc_of(a, b, node), node);
+// A tile in a wave's registers, as it is stored: 1 KB pieces, 16 bytes a lane.
+template <int DH>
+struct Keys {
+  u32x4 r[DH / 32];
+};
+template <int DH>
+struct Vals {
+  u32x4 r[DH / 32];
+};
 
-  // Q^T operands: piece x, half u holds dims 32 x + 16 hh + 8 u ..
-  f16x8 qh[KP][2], ql[SPLIT ? KP : 1][2];
-  float fac;  // scale_log2 and the row's power of two
-  {
-    float x[KP][2][8];
-    const long long o = b * a.q.sb + node * a.q.sr + hq * a.q.sh + 16 * hh;
-#pragma unroll
-    for (int p = 0; p < KP; ++p)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        load8(a.q.p, o + 32 * p + 8 * h, a.q_lo.p ? PT_BF16 : a.dtype, a.q.vec, x[p][h]);
-        if (SPLIT && a.q_lo.p) {
-          float y[8];
-          load8(a.q_lo.p, o + 32 * p + 8 * h, PT_BF16, a.q.vec, y);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) x[p][h][e] += y[e];
-        }
-      }
-    float mx = 0.f;
-#pragma unroll
-    for (int p = 0; p < KP; ++p)
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) mx = fmaxf(mx, fabsf(x[p][h][e]));
-    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-    // to [2^8, 2^9); subnormal rows stay near zero, infinite ones infinite
-    const int ex = min(max((int)(__float_as_uint(mx) >> 23) - 127, -110), 118);
-    const float f = pow2i(8 - ex);
-    fac = a.scale_log2 * pow2i(ex - 8);
-#pragma unroll
-    for (int p = 0; p < KP; ++p)
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float v = x[p][h][e] * f;
-          const _Float16 hi = (_Float16)v;
-          qh[p][h][e] = hi;
-          if constexpr (SPLIT) ql[p][h][e] = (_Float16)(v - (float)hi);
-        }
-  }
+// Q^T operand of a row tile: lane (row col, half hh) holds, of piece x and
+// half h, dims 32 x + 16 hh + 8 h .. (Q_FP8: pieces 2 y and 2 y + 1 together).
+template <int DH, int QF>
+struct Query {
+  static constexpr int KP = DH / 32;
+  u32x4 a[QF == Q_FP8 ? 1 : KP][2], b[QF == Q_SPLIT ? KP : 1][2];
+  i32x8 e[QF == Q_FP8 ? KP / 2 : 1][2];
+  float fac;  // the scores' scale in the log2 domain, and the power of two that the row was scaled by
 
-  float m = NO_MAX, l = 0.f;
-  int E = PAGED_E_MIN;
-  f32x16 oacc[DB];
+  __device__ __forceinline__ void load(const PagedAttn& p, long long at) {
+    fac = p.scale_log2;
+    if constexpr (QF == Q_BF16 || QF == Q_F16) {
 #pragma unroll
-  for (int d = 0; d < DB; ++d)
+      for (int x = 0; x < KP; ++x)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) oacc[d][r] = 0.f;
-
-  // MFMA row -> slot of the tile: row 8q + 4h + e holds slot 16h + 4q + e
-  const int krow = 16 * ((col >> 2) & 1) + 4 * (col >> 3) + (col & 3);
-  const uint32_t ko = (hh * 32 + krow) * 16, vo = col * 32 + 16 * hh;
-  const int wu = __builtin_amdgcn_readfirstlane(w);
-
-  // The wave's tiles i0 + w, i0 + w + 4, ..: lane j looks up the j-th of 64.
-  for (int base = i0 + wu; base < i1; base += 64 * NW) {
-    int my_tile = 0, my_at = 0, my_ke = 0, my_ve = 0;
-    const int my = base + NW * lane;
-    if (my < i1) {
-      my_tile = my < seq.sink ? my : my - seq.sink + seq.lo;
-      int page = a.tab.pages[(long long)b * a.tab.stride + my_tile / a.pool.tpp];
-      if (page < 0 || page >= a.pool.n_pages) {
-        bad = true;
-        if (a.status) atomicOr(a.status, PAGED_BAD_PAGE);
-        page = 0;
-      }
-      my_at = (page * a.pool.Hkv + hk) * a.pool.tpp + my_tile % a.pool.tpp;
-      my_ke = a.pool.ke[my_at];
-      my_ve = a.pool.ve[my_at];
-    }
-    const int cnt = min(64, (i1 - base + NW - 1) / NW);
-    u32x4 kf[KP], vf[DB];
-    auto load = [&](int i, u32x4 (&kr)[KP], u32x4 (&vr)[DB]) {
-      const long long o = (long long)__builtin_amdgcn_readlane(my_at, i) * (32 * DH);
-      const uint8_t *kp = a.pool.k + o, *vp = a.pool.v + o;
-#pragma unroll
-      for (int x = 0; x < KP; ++x) kr[x] = *reinterpret_cast<const u32x4*>(kp + 1024 * x + ko);
-#pragma unroll
-      for (int x = 0; x < DB; ++x) vr[x] = *reinterpret_cast<const u32x4*>(vp + 1024 * x + vo);
-    };
-    load(0, kf, vf);
-    for (int i = 0; i < cnt; ++i) {
-      u32x4 kn[KP], vn[DB];
-      load(min(i + 1, cnt - 1), kn, vn);
-      const int tile = __builtin_amdgcn_readlane(my_tile, i), s0 = tile * 32;
-      const int ke = __builtin_amdgcn_readlane(my_ke, i), ve = __builtin_amdgcn_readlane(my_ve, i);
-      f32x16 s, s2;
-#pragma unroll
-      for (int r = 0; r < 16; ++r) s[r] = s2[r] = 0.f;
+        for (int h = 0; h < 2; ++h) a[x][h] = load8_raw(p.q.p, at + 32 * x + 8 * h, p.q.vec);
+    } else {
+      float v[KP][2][8];
+      float mx = 0.f;
 #pragma unroll
       for (int x = 0; x < KP; ++x)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const f16x8 k8 = cvt8(kf[x][2 * h], kf[x][2 * h + 1], 1.f);
-          s = __builtin_amdgcn_mfma_f32_32x32x16_f16(k8, qh[x][h], s, 0, 0, 0);
-          if constexpr (SPLIT) s2 = __builtin_amdgcn_mfma_f32_32x32x16_f16(k8, ql[x][h], s2, 0, 0, 0);
-        }
-      if constexpr (SPLIT) s += s2;
-      // a tile that not every row sees whole: the last one, those at the
-      // windows' starts, and the last one of the sinks
-      const bool edge = s0 + 32 > len || (a.cut.window && s0 + 32 > a.cut.sinks && s0 < len + a.nodes - a.cut.window);
-      bool nan_v = false;
-      if (edge) {  // uniform
-        const int lo = a.cut.window ? pos - a.cut.window : -1;  // slots above it are seen
+          load8(p.q.p, at + 32 * x + 8 * h, QF == Q_FP8 || p.q_lo.p ? PT_BF16 : PT_F32, p.q.vec, v[x][h]);
+          if (QF == Q_SPLIT && p.q_lo.p) {
+            float y[8];
+            load8(p.q_lo.p, at + 32 * x + 8 * h, PT_BF16, p.q.vec, y);
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int slot = s0 + 16 * hh + r;
-          if (!(slot < len && (slot > lo || slot < a.cut.sinks))) s[r] = -INFINITY;
-        }
-      }
-      // never 0, which times a masked -inf would be a NaN
-      const float f = fmaxf(fac * pow2i(ke), 0x1p-126f);
-      float p[16];
-      auto probs = [&]() {
-        float t[16];
-#pragma unroll
-        for (int r = 0; r < 16; ++r) t[r] = p[r] = __builtin_amdgcn_exp2f(fmaf(s[r], f, -m));
-#pragma unroll
-        for (int o = 8; o > 0; o >>= 1)
-#pragma unroll
-          for (int r = 0; r < o; ++r) t[r] += t[r + o];
-        return t[0];
-      };
-      float sum = probs();
-      if (__any(sum > 16384.f)) {
-        float mx = -INFINITY;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[r]);
-        mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * f;
-        const float mn = fmaxf(m, mx), al = __builtin_amdgcn_exp2f(m - mn);
-        m = mn;
-        l *= al;
-#pragma unroll
-        for (int d = 0; d < DB; ++d) oacc[d] *= al;
-        sum = probs();
-      }
-      l += sum;
-      if (ve > E) {  // uniform
-        const float al = pow2i(E - ve);
-        E = ve;
-#pragma unroll
-        for (int d = 0; d < DB; ++d) oacc[d] *= al;
-      }
-      const float vs = pow2i(ve - E);
-      if (edge) {
-        // what lies in slots that a row does not see must not reach it, NaN
-        // included: bytes that no row sees become 0 ..
-        const int lo0 = a.cut.window ? len - a.cut.window : -1;
-#pragma unroll
-        for (int x = 0; x < DB; ++x)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            uint32_t keep = 0;
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-              const int slot = s0 + 16 * hh + 4 * e + c;
-              if (slot < len && (slot > lo0 || slot < a.cut.sinks)) keep |= 0xffu << (8 * c);
-            }
-            const uint32_t v = vf[x][e] & keep;
-            vf[x][e] = v;
-            nan_v |= (((v & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0;
+            for (int i = 0; i < 8; ++i) v[x][h][i] += y[i];
           }
-        // .. and a NaN that only some rows see is given to those (rare: a
-        // product of their 0 / 1 masks with the NaNs' places)
-        if (a.cut.window && __any(nan_v)) {
 #pragma unroll
-          for (int x = 0; x < DB; ++x) {
-            f32x16 hit;
+          for (int i = 0; i < 8; ++i) mx = fmaxf(mx, fabsf(v[x][h][i]));
+        }
+      mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+      // the row's largest value to [2^TOP, 2^(TOP + 1)); subnormal rows stay
+      // near zero, infinite ones infinite
+      constexpr int TOP = QF == Q_FP8 ? 7 : 8;
+      const int ex = min(max((int)(__float_as_uint(mx) >> 23) - 127, -110), 118);
+      const float f = pow2i(TOP - ex);
+      fac *= pow2i(ex - TOP);
 #pragma unroll
-            for (int r = 0; r < 16; ++r) hit[r] = 0.f;
+      for (int x = 0; x < KP; ++x)
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-              f16x8 is, sees;
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-              for (int e = 0; e < 8; ++e) {
-                const uint32_t byte = vf[x][2 * t + e / 4] >> (8 * (e % 4)) & 0x7f;
-                is[e] = byte == 0x7f ? (_Float16)1.f : (_Float16)0.f;
-                sees[e] = s[8 * t + e] == -INFINITY ? (_Float16)0.f : (_Float16)1.f;
+          for (int i = 0; i < 8; i += 2) {
+            const float v0 = v[x][h][i] * f, v1 = v[x][h][i + 1] * f;
+            if constexpr (QF == Q_SPLIT) {
+              const f16x2 hi = __builtin_convertvector(f32x2{v0, v1}, f16x2);
+              const f16x2 lo = __builtin_convertvector(f32x2{v0 - (float)hi.x, v1 - (float)hi.y}, f16x2);
+              a[x][h][i / 2] = __builtin_bit_cast(uint32_t, hi);
+              b[x][h][i / 2] = __builtin_bit_cast(uint32_t, lo);
+            } else {
+              // word i / 4 of the half, its lower or upper pair; the low part
+              // 2^4 up, which its product's scale takes back
+              const int at8 = 4 * (x % 2) + 2 * h + i / 4;
+              if (i % 4 == 0) {
+                const int w = __builtin_amdgcn_cvt_pk_fp8_f32(v0, v1, 0, false);
+                const f32x2 hi = __builtin_amdgcn_cvt_pk_f32_fp8(w, false);
+                e[x / 2][0][at8] = w;
+                e[x / 2][1][at8] = __builtin_amdgcn_cvt_pk_fp8_f32((v0 - hi.x) * 16.f, (v1 - hi.y) * 16.f, 0, false);
+              } else {
+                const int w = __builtin_amdgcn_cvt_pk_fp8_f32(v0, v1, e[x / 2][0][at8], true);
+                const f32x2 hi = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
+                e[x / 2][0][at8] = w;
+                e[x / 2][1][at8] = __builtin_amdgcn_cvt_pk_fp8_f32((v0 - hi.x) * 16.f, (v1 - hi.y) * 16.f, e[x / 2][1][at8], true);
               }
-              hit = __builtin_amdgcn_mfma_f32_32x32x16_f16(is, sees, hit, 0, 0, 0);
             }
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-              if (hit[r] > 0.f) oacc[x][r] = __builtin_nanf("");
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-#pragma unroll
-              for (int c = 0; c < 4; ++c)
-                if ((vf[x][e] >> (8 * c) & 0x7f) == 0x7f) vf[x][e] &= ~(0xffu << (8 * c));
           }
-        }
-      }
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        f16x8 ph, pl;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const _Float16 hi = (_Float16)p[8 * t + e];
-          ph[e] = hi;
-          if constexpr (SPLIT) pl[e] = (_Float16)(p[8 * t + e] - (float)hi);
-        }
-#pragma unroll
-        for (int x = 0; x < DB; ++x) {
-          const f16x8 v8 = cvt8(vf[x][2 * t], vf[x][2 * t + 1], vs);
-          oacc[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v8, ph, oacc[x], 0, 0, 0);
-          if constexpr (SPLIT) oacc[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v8, pl, oacc[x], 0, 0, 0);
-        }
-      }
-#pragma unroll
-      for (int x = 0; x < KP; ++x) kf[x] = kn[x];
-#pragma unroll
-      for (int x = 0; x < DB; ++x) vf[x] = vn[x];
     }
   }
-  l += __shfl_xor(l, 32, 64);
-  if (__any(bad)) l = __builtin_nanf("");  // a tile that is not there: the rows become NaN
 
-  // ---- the waves' results meet in LDS: row `col` at so[w][col * DH ..], its
-  // 16-byte chunk c at c ^ (col & 7)
-  {
-    const float fe = pow2i(E);
-#pragma unroll
-    for (int d = 0; d < DB; ++d)
-#pragma unroll
-      for (int rg = 0; rg < 4; ++rg) {
-        const int c = 8 * d + 2 * rg + hh;
-        *reinterpret_cast<float4*>(&so[w][col * DH + 4 * (c ^ (col & 7))]) =
-            make_float4(oacc[d][4 * rg] * fe, oacc[d][4 * rg + 1] * fe, oacc[d][4 * rg + 2] * fe, oacc[d][4 * rg + 3] * fe);
-      }
-    if (hh == 0) sm[w][col] = m, sl[w][col] = l;
+  // S^T = K Q^T: what step g of STEPS adds to hi (and lo, the low part's sum
+  // of Q_SPLIT), given the keys and, of those that have to be converted, piece
+  // g / PER's halves
+  static constexpr int STEPS = QF == Q_FP8 ? KP : QF == Q_SPLIT ? 4 * KP : 2 * KP;
+  __device__ __forceinline__ void step(int g, const Keys<DH>& k, const u32x4& k16, f32x16& hi, f32x16& lo) const {
+    if constexpr (QF == Q_FP8) {
+      const i32x8 k8 = __builtin_bit_cast(i32x8, KeyPair{k.r[g / 2 * 2], k.r[g / 2 * 2 + 1]});
+      hi = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k8, e[g / 2][g % 2], hi, 0, 0, 0, 0x7f7f7f7f, 0,
+                                                           g % 2 ? 0x7b7b7b7b : 0x7f7f7f7f);
+    } else if constexpr (QF == Q_BF16) {
+      hi = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(k16), as_bf16x8(a[g / 2][g % 2]), hi, 0, 0, 0);
+    } else if constexpr (QF == Q_F16) {
+      hi = __builtin_amdgcn_mfma_f32_32x32x16_f16(as_f16x8(k16), as_f16x8(a[g / 2][g % 2]), hi, 0, 0, 0);
+    } else if (g % 2 == 0) {
+      hi = __builtin_amdgcn_mfma_f32_32x32x16_f16(as_f16x8(k16), as_f16x8(a[g / 4][g / 2 % 2]), hi, 0, 0, 0);
+    } else {
+      lo = __builtin_amdgcn_mfma_f32_32x32x16_f16(as_f16x8(k16), as_f16x8(b[g / 4][g / 2 % 2]), lo, 0, 0, 0);
+    }
   }
+  // the converted keys of step g (the same for a Q_SPLIT pair)
+  static __device__ __forceinline__ u32x4 convert(int g, const Keys<DH>& k) {
+    const int c = QF == Q_SPLIT ? g / 2 : g;
+    const uint32_t x = k.r[c / 2][2 * (c % 2)], y = k.r[c / 2][2 * (c % 2) + 1];
+    if constexpr (QF == Q_BF16) return __builtin_bit_cast(u32x4, cvt8_bf16(x, y));
+    else return __builtin_bit_cast(u32x4, cvt8(x, y, 1.f));
+  }
+  __device__ __forceinline__ f32x16 scores(const Keys<DH>& k) const {
+    f32x16 hi = f32x16(0.f), lo = f32x16(0.f);
+    u32x4 k16 = zero_u4();
+#pragma unroll
+    for (int g = 0; g < STEPS; ++g) {
+      if (QF != Q_FP8 && (QF != Q_SPLIT || g % 2 == 0)) k16 = convert(g, k);
+      step(g, k, k16, hi, lo);
+    }
+    if constexpr (QF == Q_SPLIT) hi += lo;
+    return hi;
+  }
+};
+
+// Running softmax and output of a row tile: lane col's row (both halves hold
+// it), dims 32 d + 8 (r / 4) + 4 hh + r % 4 of it in o[d][r], times 2^-E.
+template <int DH>
+struct State {
+  float m, l;
+  int E;  // uniform
+  f32x16 o[DH / 32];
+
+  __device__ __forceinline__ void clear() {
+    m = NO_MAX;
+    l = 0.f;
+    E = PAGED_E_MIN;
+#pragma unroll
+    for (int d = 0; d < DH / 32; ++d) o[d] = f32x16(0.f);
+  }
+  __device__ __forceinline__ void scale(float f) {
+#pragma unroll
+    for (int d = 0; d < DH / 32; ++d) o[d] *= f;
+  }
+  // raise the reference to the scores' maximum (both halves')
+  __device__ __forceinline__ void follow(const f32x16& s, float f) {
+    float mx = -INFINITY;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[r]);
+    mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * f;
+    const float mn = fmaxf(m, mx), al = __builtin_amdgcn_exp2f(m - mn);
+    m = mn;
+    l *= al;
+    scale(al);
+  }
+  // raise E to a tile's exponent
+  __device__ __forceinline__ void reach(int ve) {
+    if (ve > E) {  // uniform
+      scale(pow2i(E - ve));
+      E = ve;
+    }
+  }
+};
+
+// A score's factor on a tile: never 0, which times a masked -inf would be a NaN.
+__device__ __forceinline__ float score_factor(float fac, int ke) { return fmaxf(fac * pow2i(ke), 0x1p-126f); }
+
+// The places of a tile that a row does not see, for lane half hh.
+struct Sight {
+  int len, window, sinks;
+  __device__ __forceinline__ bool of(int slot, int pos) const {
+    return slot < len && (window == 0 || slot > pos - window || slot < sinks);
+  }
+};
+
+struct Edge {
+  static constexpr bool value = true;
+};
+struct Whole {
+  static constexpr bool value = false;
+};
+
+// Softmax of one tile's scores and O^T += V^T P^T.  EDGE: a tile (first slot
+// s0) that not every row sees whole; this lane's row stands at `pos`, the
+// first node at sight.len.
+template <int DH, int QF, class EDGE>
+__device__ __forceinline__ void attend(State<DH>& st, f32x16 s, Vals<DH> v, float f, int ve, EDGE, const Sight& sight,
+                                       int s0, int pos) {
+  constexpr int DB = DH / 32;
+  const int hh = threadIdx.x >> 5 & 1;
+  if constexpr (EDGE::value) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+      if (!sight.of(s0 + 16 * hh + r, pos)) s[r] = -INFINITY;
+  }
+  float p[16], sum;
+  auto probs = [&]() {
+    float x[8];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) p[r] = __builtin_amdgcn_exp2f(fmaf(s[r], f, -st.m));
+#pragma unroll
+    for (int r = 0; r < 8; ++r) x[r] = p[r] + p[r + 8];
+#pragma unroll
+    for (int o = 4; o > 0; o >>= 1)
+#pragma unroll
+      for (int r = 0; r < o; ++r) x[r] += x[r + o];
+    sum = x[0];
+  };
+  probs();
+  if (__any(sum > 16384.f)) {
+    st.follow(s, f);
+    probs();
+  }
+  st.l += sum;
+  st.reach(ve);
+  const float vs = pow2i(ve - st.E);
+  if constexpr (EDGE::value) {
+    // what lies in slots that a row does not see must not reach it, NaN
+    // included: bytes that no row sees become 0 ..
+    bool nan_v = false;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      uint32_t keep = 0;
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        if (sight.of(s0 + 16 * hh + 4 * e + c, sight.len)) keep |= 0xffu << (8 * c);
+#pragma unroll
+      for (int x = 0; x < DB; ++x) {
+        const uint32_t y = v.r[x][e] & keep;
+        v.r[x][e] = y;
+        nan_v |= (((y & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0;
+      }
+    }
+    // .. and a NaN that only some rows see is given to those (rare: a product
+    // of their 0 / 1 masks with the NaNs' places)
+    if (sight.window && __any(nan_v)) {
+#pragma unroll
+      for (int x = 0; x < DB; ++x) {
+        f32x16 hit = f32x16(0.f);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          f16x8 is, sees;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const uint32_t byte = v.r[x][2 * h + e / 4] >> (8 * (e % 4)) & 0x7f;
+            is[e] = byte == 0x7f ? (_Float16)1.f : (_Float16)0.f;
+            sees[e] = s[8 * h + e] == -INFINITY ? (_Float16)0.f : (_Float16)1.f;
+          }
+          hit = __builtin_amdgcn_mfma_f32_32x32x16_f16(is, sees, hit, 0, 0, 0);
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (hit[r] > 0.f) st.o[x][r] = __builtin_nanf("");
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+            if ((v.r[x][e] >> (8 * c) & 0x7f) == 0x7f) v.r[x][e] &= ~(0xffu << (8 * c));
+      }
+    }
+  }
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    u32x4 ph, pl;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float x = p[8 * h + 2 * e], y = p[8 * h + 2 * e + 1];
+      const f16x2 hi = __builtin_convertvector(f32x2{x, y}, f16x2);
+      ph[e] = __builtin_bit_cast(uint32_t, hi);
+      if constexpr (probs_split(QF))
+        pl[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{x - (float)hi.x, y - (float)hi.y}, f16x2));
+    }
+#pragma unroll
+    for (int x = 0; x < DB; ++x) {
+      const f16x8 v8 = cvt8(v.r[x][2 * h], v.r[x][2 * h + 1], vs);
+      st.o[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v8, as_f16x8(ph), st.o[x], 0, 0, 0);
+      if constexpr (probs_split(QF)) st.o[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v8, as_f16x8(pl), st.o[x], 0, 0, 0);
+    }
+  }
+}
+
+// Where a workgroup works: unit u (sequence b, the list's tiles [i0, i1)) of KV
+// head hk, row block rb.
+struct Place {
+  int u, b, hk, rb, i0, i1;
+  SeqTiles seq;
+  Sight sight;
+  bool bad;
+};
+__device__ __forceinline__ bool place_of(const PagedAttn& a, int blocks, Place& p) {
+  // XCD-aware decode: workgroups go round-robin over the 8 XCDs, so the row
+  // blocks of one (unit, KV head) get the same id % 8 and share its L2
+  const int id = blockIdx.x, rest = id >> 3;
+  p.rb = rest % blocks;
+  const int st = (rest / blocks) * 8 + (id & 7);
+  p.hk = st % a.pool.Hkv;
+  p.u = st / a.pool.Hkv;
+  const UnitAt at = unit_at(a, p.u);
+  if (at.b < 0) return false;  // uniform
+  p.b = at.b;
+  p.bad = false;
+  const int len = checked_len(a.tab, at.b, &p.bad);
+  p.seq = seq_tiles(len, a.cut);
+  p.i0 = (int)((long long)p.seq.n * at.split / at.n);
+  p.i1 = (int)((long long)p.seq.n * (at.split + 1) / at.n);
+  p.sight = Sight{len, a.cut.window, a.cut.sinks};
+  // the joining kernel finds a sequence's units here
+  if (at.split == 0 && p.hk == 0 && p.rb == 0 && threadIdx.x == 0) a.first_unit[at.b] = make_int2(p.u, at.n);
+  return true;
+}
+
+// The tile that entry i of a sequence's list is, and its number in the pool.
+struct TileAt {
+  int tile, at;
+};
+__device__ __forceinline__ TileAt look_up(const PagedAttn& a, Place& p, int i) {
+  TileAt t;
+  t.tile = i < p.seq.sink ? i : i - p.seq.sink + p.seq.lo;
+  int page = a.tab.pages[(long long)p.b * a.tab.stride + t.tile / a.pool.tpp];
+  if (page < 0 || page >= a.pool.n_pages) {
+    p.bad = true;
+    if (a.status) atomicOr(a.status, PAGED_BAD_PAGE);
+    page = 0;
+  }
+  t.at = (page * a.pool.Hkv + p.hk) * a.pool.tpp + t.tile % a.pool.tpp;
+  return t;
+}
+
+// MFMA row -> slot of the tile: row 8q + 4h + e holds slot 16h + 4q + e
+__device__ __forceinline__ int slot_of_row(int col) { return 16 * ((col >> 2) & 1) + 4 * (col >> 3) + (col & 3); }
+
+template <int DH>
+__device__ __forceinline__ void load_keys(const PagedAttn& a, long long at, int col, int hh, Keys<DH>& k) {
+  const uint8_t* p = a.pool.k + at * (32 * DH) + (hh * 32 + slot_of_row(col)) * 16;
+#pragma unroll
+  for (int x = 0; x < DH / 32; ++x) k.r[x] = *reinterpret_cast<const u32x4*>(p + 1024 * x);
+}
+template <int DH>
+__device__ __forceinline__ void load_vals(const PagedAttn& a, long long at, int col, int hh, Vals<DH>& v) {
+  const uint8_t* p = a.pool.v + at * (32 * DH) + col * 32 + 16 * hh;
+#pragma unroll
+  for (int x = 0; x < DH / 32; ++x) v.r[x] = *reinterpret_cast<const u32x4*>(p + 1024 * x);
+}
+
+// A row tile's output to LDS: row r at buf[r * DH ..], its 16-byte chunk c at
+// c ^ (r & 7) (conflict-free here and where rows are read).
+template <int DH>
+__device__ __forceinline__ void put_rows(const State<DH>& st, int col, int hh, float* buf) {
+  const float fe = pow2i(st.E);
+#pragma unroll
+  for (int d = 0; d < DH / 32; ++d)
+#pragma unroll
+    for (int rg = 0; rg < 4; ++rg) {
+      const int c = 8 * d + 2 * rg + hh;
+      *reinterpret_cast<float4*>(buf + col * DH + 4 * (c ^ (col & 7))) =
+          make_float4(st.o[d][4 * rg] * fe, st.o[d][4 * rg + 1] * fe, st.o[d][4 * rg + 2] * fe, st.o[d][4 * rg + 3] * fe);
+    }
+}
+
+// One row tile per workgroup, whose four waves take every fourth tile of the
+// unit each and meet in LDS.  Two workgroups per CU; the next tile's loads are
+// in flight while one is computed.
+template <int DH, int QF>
+__global__ __launch_bounds__(256, 2) void paged_attention_kernel(PagedAttn a) {
+  constexpr int NW = 4;
+  __shared__ float so[NW][32 * DH];
+  __shared__ float sm[NW][32], sl[NW][32];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = lane & 31, hh = lane >> 5;
+  const int G = a.Hq / a.pool.Hkv, R = G * a.nodes;
+  Place p;
+  if (!place_of(a, (R + 31) / 32, p)) return;
+  const int count = a.counts ? a.counts[p.b] : a.nodes;
+
+  // lane j looks up the j-th of 64 of the wave's tiles i0 + w, i0 + w + 4, ..
+  const int mine = p.i1 - p.i0 - w > 0 ? (p.i1 - p.i0 - w + NW - 1) / NW : 0;
+  int my_tile = 0, my_at = 0, my_ke = 0, my_ve = 0;
+  auto look = [&](int base) {
+    if (base + lane < mine) {
+      const TileAt t = look_up(a, p, p.i0 + w + NW * (base + lane));
+      my_tile = t.tile;
+      my_at = t.at;
+      my_ke = a.pool.ke[t.at];
+      my_ve = a.pool.ve[t.at];
+    }
+  };
+  look(0);
+  const int row = min(p.rb * 32 + col, R - 1), node = row % a.nodes, hq = p.hk * G + row / a.nodes;
+  const int pos = a.cut.window ? p.sight.len + depth_of(anc_of(a, p.b, node), node) : 0;
+  Query<DH, QF> q;
+  q.load(a, p.b * a.q.sb + node * a.q.sr + hq * a.q.sh + 16 * hh);
+  State<DH> st;
+  st.clear();
+  for (int base = 0; base < mine; base += 64) {
+    if (base) look(base);
+    // tiles that not every row sees whole (the last one, those at the windows'
+    // starts, the last one of the sinks) come first
+    const int s0 = my_tile * 32;
+    const bool edge = s0 + 32 > p.sight.len ||
+                      (a.cut.window && s0 + 32 > a.cut.sinks && s0 < p.sight.len + a.nodes - a.cut.window);
+    const unsigned long long all = __ballot(base + lane < mine);
+    unsigned long long todo = all & __ballot(edge), rest = all & ~todo;
+    Keys<DH> k0, k1;
+    Vals<DH> v0, v1;
+    auto load = [&](int i, Keys<DH>& k, Vals<DH>& v) {
+      const long long at = __builtin_amdgcn_readlane(my_at, i);
+      load_keys<DH>(a, at, col, hh, k);
+      load_vals<DH>(a, at, col, hh, v);
+    };
+    auto tile = [&](auto kind, int i, const Keys<DH>& k, const Vals<DH>& v) {
+      const f32x16 s = q.scores(k);
+      attend<DH, QF>(st, s, v, score_factor(q.fac, __builtin_amdgcn_readlane(my_ke, i)),
+                     __builtin_amdgcn_readlane(my_ve, i), kind, p.sight, __builtin_amdgcn_readlane(my_tile, i) * 32, pos);
+    };
+    while (todo) {
+      const int i = __builtin_ctzll(todo);
+      todo &= todo - 1;
+      load(i, k0, v0);
+      tile(Edge{}, i, k0, v0);
+    }
+    if (!rest) continue;
+    int left = __builtin_popcountll(rest);
+    auto next = [&](int i) {  // the next of the others, or the last one again
+      const unsigned long long r = rest;
+      rest &= rest - 1;
+      return r ? (int)__builtin_ctzll(r) : i;
+    };
+    int i = next(0);
+    load(i, k0, v0);
+    for (;;) {
+      const int n = next(i);
+      load(n, k1, v1);
+      tile(Whole{}, i, k0, v0);
+      if (--left == 0) break;
+      i = next(n);
+      load(i, k0, v0);
+      tile(Whole{}, n, k1, v1);
+      if (--left == 0) break;
+    }
+  }
+  float l = st.l + __shfl_xor(st.l, 32, 64);
+  if (__any(p.bad)) l = __builtin_nanf("");  // a tile that is not there: the rows become NaN
+  put_rows<DH>(st, col, hh, so[w]);
+  if (hh == 0) sm[w][col] = st.m, sl[w][col] = l;
   __syncthreads();
   constexpr int CH = DH / 4;
-  const long long prow = ((long long)u * a.pool.Hkv + hk) * R + rt * 32;
-  const int live = min(32, R - rt * 32);
+  const long long prow = ((long long)p.u * a.pool.Hkv + p.hk) * R + p.rb * 32;
+  const int live = min(32, R - p.rb * 32);
   for (int i = threadIdx.x; i < live * CH; i += 256) {
     const int r = i / CH, c = i % CH;
-    if ((rt * 32 + r) % a.nodes >= count) continue;  // an absent node
+    if ((p.rb * 32 + r) % a.nodes >= count) continue;  // an absent node
     float M = sm[0][r];
 #pragma unroll
     for (int x = 1; x < NW; ++x) M = fmaxf(M, sm[x][r]);
@@ -426,45 +597,307 @@ __global__ __launch_bounds__(256, 2) void paged_attention_kernel(PagedAttn a) {
       L += f * sl[x][r];
     }
     *reinterpret_cast<float4*>(a.part_o + (prow + r) * DH + 4 * c) = o;
-    if (c == 0) a.part_ml[(prow + r) * 2] = M, a.part_ml[(prow + r) * 2 + 1] = L;
+    if (c == 0) *reinterpret_cast<float2*>(a.part_ml + (prow + r) * 2) = make_float2(M, L);
   }
 }
 
-// A thread: 4 dims of a head of one node.
+// Row tiles side by side: NW waves of one row tile each over the same tiles,
+// which the workgroup stages into an LDS ring once (each wave an equal share of
+// a tile's 1 KB pieces, which are MFMA operands as they stand).  Two waves per
+// SIMD; a step over tile i is written as a sequence of MFMAs with their share
+// of everything else, held by sched_barrier, so that matrix and vector work
+// overlap:
+//   the scores of tile i + 1, between the softmax of tile i;
+//   O += V P of tile i, between the conversion of its values, the reads of tile
+//   i + 2's keys and the maximum of tile i + 1's scores, which decides whether
+//   a reference has to rise: no branch stands inside a step.
+// The workgroup meets once in two tiles (2 p, 2 p + 1): then every wave has its
+// share of pair p + 2 and is done with pair p, whose slots pair p + D / 2 gets.
+// Tiles that not every row sees whole are computed one by one before.
+template <int DH, int QF, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void paged_wide_kernel(PagedAttn a) {
+  constexpr int KP = DH / 32, DB = DH / 32, PIECES = KP + DB, D = 2 * NW;  // ring slots
+  constexpr int STAGERS = PIECES < NW ? PIECES : NW, PPW = PIECES / STAGERS;  // waves that stage, pieces of each
+  static_assert(PIECES % STAGERS == 0 && PPW * D < 64 && D % 2 == 0 && D >= 8, "ring shape");
+  constexpr int LDS = D * PIECES * 1024 > NW * 32 * DH * 4 ? D * PIECES * 1024 : NW * 32 * DH * 4;
+  __shared__ u32x4 lds[LDS / 16];
+  u32x4(*ring)[PIECES][64] = reinterpret_cast<u32x4(*)[PIECES][64]>(lds);
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = lane & 31, hh = lane >> 5;
+  const int G = a.Hq / a.pool.Hkv, R = G * a.nodes;
+  Place p;
+  if (!place_of(a, (R + 32 * NW - 1) / (32 * NW), p)) return;
+  const int count = a.counts ? a.counts[p.b] : a.nodes;
+  const int row0 = (p.rb * NW + w) * 32;
+
+  // The unit's tiles that every row sees whole: list entries [i0, e0) and
+  // [w0, w1); the others are [e0, w0) and [w1, i1).
+  int e0 = p.i0, w0 = p.i0, w1 = p.i1;
+  {
+    const int len = p.sight.len;
+    if (a.cut.window) {
+      e0 = min(max(min(p.seq.sink, a.cut.sinks >> 5), p.i0), p.i1);
+      const int clear = max(0, len + a.nodes - a.cut.window);  // slots from here on are in every window
+      w0 = max(p.seq.sink, ((clear + 31) >> 5) - p.seq.lo + p.seq.sink);
+      w0 = min(max(w0, e0), p.i1);
+    }
+    w1 = min(max(p.seq.n - ((len & 31) != 0), w0), p.i1);
+  }
+  const int n0 = e0 - p.i0, whole = n0 + w1 - w0, edges = p.i1 - p.i0 - whole;
+  auto whole_at = [&](int j) { return j < n0 ? p.i0 + j : w0 + j - n0; };
+  auto edge_at = [&](int j) { return j < w0 - e0 ? e0 + j : w1 + j - (w0 - e0); };
+
+  const int row = min(row0 + col, R - 1), node = row % a.nodes, hq = p.hk * G + row / a.nodes;
+  const int pos = a.cut.window ? p.sight.len + depth_of(anc_of(a, p.b, node), node) : 0;
+  Query<DH, QF> q;
+  q.load(a, p.b * a.q.sb + node * a.q.sr + hq * a.q.sh + 16 * hh);
+  State<DH> st;
+  st.clear();
+  for (int j = 0; j < edges; ++j) {
+    const TileAt x = look_up(a, p, edge_at(j));
+    Keys<DH> k;
+    Vals<DH> v;
+    load_keys<DH>(a, x.at, col, hh, k);
+    load_vals<DH>(a, x.at, col, hh, v);
+    const int ke = __builtin_amdgcn_readfirstlane(a.pool.ke[x.at]), ve = __builtin_amdgcn_readfirstlane(a.pool.ve[x.at]);
+    attend<DH, QF>(st, q.scores(k), v, score_factor(q.fac, ke), ve, Edge{}, p.sight, x.tile * 32, pos);
+  }
+
+  if (whole > 0) {  // uniform over the workgroup
+    // tile j's pool number, and 2^ke (a float) with ve in its low byte: lane
+    // j % 64 of one of two banks
+    int at0 = 0, at1 = 0, ex0 = 0, ex1 = 0;
+    auto fill = [&](int c) {  // tiles 64 c .. into bank c % 2
+      const int j = 64 * c + lane;
+      int at = 0, e = 0;
+      if (j < whole) {
+        at = look_up(a, p, whole_at(j)).at;
+        e = (int)(__float_as_uint(pow2i(a.pool.ke[at])) | (uint8_t)a.pool.ve[at]);
+      }
+      at0 = c & 1 ? at0 : at;
+      ex0 = c & 1 ? ex0 : e;
+      at1 = c & 1 ? at : at1;
+      ex1 = c & 1 ? e : ex1;
+    };
+    fill(0);
+    fill(1);
+    auto of = [](int x0, int x1, int j) {
+      const int y0 = __builtin_amdgcn_readlane(x0, j & 63), y1 = __builtin_amdgcn_readlane(x1, j & 63);
+      return j >> 6 & 1 ? y1 : y0;
+    };
+    // this lane's byte offset inside a tile, for each piece this wave stages
+    const bool stager = w < STAGERS;
+    uint32_t goff[PPW];
+#pragma unroll
+    for (int x = 0; x < PPW; ++x) {
+      const int pc = w * PPW + x;
+      goff[x] = pc < KP ? 1024 * pc + (hh * 32 + slot_of_row(col)) * 16 : 1024 * (pc - KP) + col * 32 + 16 * hh;
+    }
+    auto issue = [&](int slot, int j) {
+      const long long at = of(at0, at1, min(j, whole - 1));
+      if (stager) {  // uniform over the wave
+#pragma unroll
+        for (int x = 0; x < PPW; ++x) {
+          const int pc = w * PPW + x;
+          const uint8_t* t = (pc < KP ? a.pool.k : a.pool.v) + at * (32 * DH);
+          __builtin_amdgcn_global_load_lds((const void*)(t + goff[x]), (lds_void*)&ring[slot][pc][0], 16, 0, 0);
+        }
+      }
+    };
+#pragma unroll
+    for (int i = 0; i < D; ++i) issue(i, i);
+
+    constexpr int SQ = Query<DH, QF>::STEPS;
+    Keys<DH> kf;
+    auto read_k = [&](int slot) {
+#pragma unroll
+      for (int x = 0; x < KP; ++x) kf.r[x] = ring[slot][x][lane];
+    };
+    // a tile's factor of the scores, and whether its scores or its values'
+    // exponent go beyond what the state refers to
+    auto factor = [&](int ex) { return fmaxf(q.fac * __int_as_float(ex & 0x7f800000), 0x1p-126f); };
+    auto beyond = [&](float mx, float f, int ex) { return __any(fmaf(mx, f, -st.m) > 14.f) || (int8_t)ex > st.E; };
+    f32x16 sa, sb;
+    wait_vmcnt_lds<(D - 4) * PPW>();  // pairs 0 and 1
+    __builtin_amdgcn_s_barrier();
+    read_k(0);
+    sa = q.scores(kf);
+    int ex = of(ex0, ex1, 0);  // of the current tile
+    float f = factor(ex);
+    bool far;
+    {
+      float mx = sa[0];
+#pragma unroll
+      for (int r = 1; r < 16; ++r) mx = fmaxf(mx, sa[r]);
+      far = beyond(mx, f, ex);
+    }
+    read_k(1);  // of a single tile: a repeat of it
+    int slot = 0;  // i % D
+    // tile i: scores s in, the next tile's out; its values in the ring's slot
+    auto step = [&](const f32x16& s, f32x16& sn, int i) {
+      if (far) {
+        st.follow(s, f);
+        st.reach((int8_t)ex);
+      }
+      const float vs = pow2i((int8_t)ex - st.E);
+      const int s1 = slot + 1 == D ? 0 : slot + 1, s2 = s1 + 1 == D ? 0 : s1 + 1;
+      const int exn = of(ex0, ex1, min(i + 1, whole - 1));
+      const float fn = factor(exn);
+      float pr[16], part[4], mx = 0.f;
+      u32x4 ph[2], pl[2];  // halves of the lane's slots
+      Vals<DH> v;
+      // softmax of slot r: the sum as a tree over the 16
+      auto prob = [&](int r) {
+        pr[r] = __builtin_amdgcn_exp2f(fmaf(s[r], f, -st.m));
+        float x = pr[r];
+        int level = 0;
+#pragma unroll
+        for (; r >> level & 1; ++level) x = part[level] + x;
+        if (level == 4) st.l += x;
+        else part[level] = x;
+        if (r & 1) {
+          const f16x2 hi = __builtin_convertvector(f32x2{pr[r - 1], pr[r]}, f16x2);
+          ph[r / 8][r / 2 % 4] = __builtin_bit_cast(uint32_t, hi);
+          if constexpr (probs_split(QF))
+            pl[r / 8][r / 2 % 4] =
+                __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{pr[r - 1] - (float)hi.x, pr[r] - (float)hi.y}, f16x2));
+        }
+      };
+      f32x16 lo = f32x16(0.f);
+      sn = f32x16(0.f);
+      u32x4 k16 = zero_u4();
+#pragma unroll
+      for (int g = 0; g < SQ; ++g) {
+        if (QF != Q_FP8 && (QF != Q_SPLIT || g % 2 == 0)) k16 = Query<DH, QF>::convert(g, kf);
+        q.step(g, kf, k16, sn, lo);
+#pragma unroll
+        for (int x = g * DB / SQ; x < (g + 1) * DB / SQ; ++x) v.r[x] = ring[slot][KP + x][lane];
+#pragma unroll
+        for (int r = g * 16 / SQ; r < (g + 1) * 16 / SQ; ++r) prob(r);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if constexpr (QF == Q_SPLIT) sn += lo;
+      constexpr int PL = probs_split(QF) ? 2 : 1, S2 = 2 * DB * PL;  // O += V P: half, dims, part
+      constexpr int S3 = S2 - 2;                                     // the maximum is there two MFMAs before the end
+      u32x4 v16 = zero_u4();
+#pragma unroll
+      for (int g = 0; g < S2; ++g) {
+        const int h = g / (DB * PL), d = g / PL % DB;
+        if (g % PL == 0) v16 = __builtin_bit_cast(u32x4, cvt8(v.r[d][2 * h], v.r[d][2 * h + 1], vs));
+        st.o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(as_f16x8(v16), as_f16x8(g % PL ? pl[h] : ph[h]), st.o[d], 0, 0, 0);
+        if (g < KP) kf.r[g] = ring[s2][g][lane];
+        if (g < S3) {
+#pragma unroll
+          for (int y = g * 16 / S3; y < (g + 1) * 16 / S3; ++y) mx = y ? fmaxf(mx, sn[y]) : sn[0];
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      far = beyond(mx, fn, exn);
+      f = fn;
+      ex = exn;
+      slot = s1;
+    };
+    for (int i = 0;; i += 2) {
+      // every tile that is still to be issued, and the current ones, are in the banks
+      if ((i & 63) == 0 && i > 0) fill((i >> 6) + 1);
+      step(sa, sb, i);
+      if (i + 1 >= whole) break;
+      step(sb, sa, i + 1);
+      if (i + 2 >= whole) break;
+      wait_vmcnt_lds<(D - 6) * PPW>();
+      __builtin_amdgcn_s_barrier();
+      const int s0 = slot >= 2 ? slot - 2 : slot + D - 2;
+      issue(s0, i + D);
+      issue(s0 + 1, i + 1 + D);
+    }
+    wait_vmcnt_lds<0>();
+  }
+  const bool hurt = __any(p.bad);
+  constexpr int CH = DH / 4, RPI = 64 / CH;  // 16-byte chunks of a row, rows per wave-wide store
+  const long long prow = ((long long)p.u * a.pool.Hkv + p.hk) * R + row0;
+  float* buf = reinterpret_cast<float*>(lds) + w * 32 * DH;
+  __syncthreads();  // every wave has left the ring
+  float l = st.l + __shfl_xor(st.l, 32, 64);
+  if (hurt) l = __builtin_nanf("");
+  put_rows<DH>(st, col, hh, buf);
+  auto live = [&](int r) { return row0 + r < R && (row0 + r) % a.nodes < count; };
+  if (hh == 0 && live(col)) *reinterpret_cast<float2*>(a.part_ml + (prow + col) * 2) = make_float2(st.m, l);
+#pragma unroll 4
+  for (int n = 0; n < 32 / RPI; ++n) {
+    const int r = n * RPI + lane / CH, c = lane % CH;
+    if (live(r))
+      *reinterpret_cast<float4*>(a.part_o + (prow + r) * DH + 4 * c) =
+          *reinterpret_cast<const float4*>(buf + r * DH + 4 * (c ^ (r & 7)));
+  }
+}
+
+// A thread: 4 dims of a head of one node.  What a row needs first (lengths,
+// masks, q, its units' place) is asked for at once, and of the root path and
+// the units eight each at a time.
 __global__ __launch_bounds__(256) void paged_combine_kernel(PagedAttn a) {
   const int dh = a.pool.dh, quads = dh / 4;
   const int b = blockIdx.x / a.nodes, i = blockIdx.x % a.nodes;
   const int t = blockIdx.y * 256 + threadIdx.x;
-  const int per = tiles_per_unit(a);
-  const Units un = units_of(a, per, b);
   const int G = a.Hq / a.pool.Hkv, R = G * a.nodes;
+  if (t >= a.Hq * quads) return;  // whole heads: 64 threads of a wave hold 2 or 4
+  const int h = t / quads, d = t % quads * 4, hk = h / G;
+  uint64_t anc = anc_of(a, b, i);
+  const int2 un = a.units > 0 ? a.first_unit[b] : make_int2(0, 0);
   bool bad = false;
   const int len = checked_len(a.tab, b, &bad);
   int count = a.counts ? a.counts[b] : a.nodes;
+  float4 q = load4(a.q.p, b * a.q.sb + i * a.q.sr + h * a.q.sh + d, a.q_lo.p ? PT_BF16 : a.dtype, a.q.vec);
+  if (a.q_lo.p) {
+    const float4 y = load4(a.q_lo.p, b * a.q.sb + i * a.q.sr + h * a.q.sh + d, PT_BF16, a.q.vec);
+    q.x += y.x, q.y += y.y, q.z += y.z, q.w += y.w;
+  }
   if (count < 0 || count > a.nodes) bad = true, count = min(max(count, 0), a.nodes);
   if (bad && a.status && threadIdx.x == 0) atomicOr(a.status, PAGED_BAD_LENGTH);
-  if (t >= a.Hq * quads) return;  // whole heads: 64 threads of a wave hold 2 or 4
-  const int h = t / quads, d = t % quads * 4, hk = h / G;
   const bool live = i < count;
   if (!live && a.out_ks == 0) return;
   float4 out = make_float4(0.f, 0.f, 0.f, 0.f);
   if (live) {  // uniform over the workgroup
-    float4 q = load4(a.q.p, b * a.q.sb + i * a.q.sr + h * a.q.sh + d, a.q_lo.p ? PT_BF16 : a.dtype, a.q.vec);
-    if (a.q_lo.p) {
-      const float4 y = load4(a.q_lo.p, b * a.q.sb + i * a.q.sr + h * a.q.sh + d, PT_BF16, a.q.vec);
-      q.x += y.x, q.y += y.y, q.z += y.z, q.w += y.w;
-    }
-    // nodes of the root path, eight at a time
-    uint64_t anc = anc_of(a, b, i);
     const int dep = depth_of(anc, i);
     float m = -INFINITY, l = 0.f;
     float4 o = out;
+    constexpr int TB = 8;
+    // the cached part's units, in their order; a sequence without tiles has
+    // none (and nobody wrote their place)
+    const int units = seq_tiles(len, a.cut).n > 0 ? un.y : 0;
+    const long long row = ((long long)un.x * a.pool.Hkv + hk) * R + (h % G) * a.nodes + i;
+    const long long step = (long long)a.pool.Hkv * R;
+    for (int s = 0; s < units; s += TB) {
+      float2 ml[TB];
+      float4 ou[TB];
+#pragma unroll
+      for (int x = 0; x < TB; ++x) {
+        const long long at = row + min(s + x, units - 1) * step;
+        ml[x] = *reinterpret_cast<const float2*>(a.part_ml + at * 2);
+        ou[x] = *reinterpret_cast<const float4*>(a.part_o + at * dh + d);
+      }
+      float mn = m;
+#pragma unroll
+      for (int x = 0; x < TB; ++x)
+        if (s + x < units && !(ml[x].x == NO_MAX && ml[x].y == 0.f)) mn = fmaxf(mn, ml[x].x);
+      if (mn == -INFINITY) continue;  // no slot of them is seen
+      const float al = exp2f(m - mn);
+      l *= al;
+      o.x *= al, o.y *= al, o.z *= al, o.w *= al;
+#pragma unroll
+      for (int x = 0; x < TB; ++x)
+        if (s + x < units) {
+          const float e = exp2f(ml[x].x - mn);
+          l += e * ml[x].y;
+          o.x += e * ou[x].x, o.y += e * ou[x].y, o.z += e * ou[x].z, o.w += e * ou[x].w;
+        }
+      m = mn;
+    }
+    // nodes of the root path
     const long long kb = b * a.k.sb + hk * a.k.sh + d, vb = b * a.v.sb + hk * a.v.sh + d;
     int r = 0;  // rank of the next node
     while (anc) {
-      constexpr int TB = 8;
+      float4 k4[TB], v4[TB];
       float sc[TB];
-      float4 v4[TB];
       int n = 0;
 #pragma unroll
       for (int x = 0; x < TB; ++x) {
@@ -473,22 +906,23 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(PagedAttn a) {
         anc &= anc - 1;
         const bool sees = ok && (!a.cut.window || dep - r < a.cut.window || (long long)len + r < a.cut.sinks);
         r += ok;
-        sc[x] = -INFINITY;
-        v4[x] = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (sees) {  // uniform
-          const float4 k = load4(a.k.p, kb + j * a.k.sr, a.dtype, a.k.vec);
-          v4[x] = load4(a.v.p, vb + j * a.v.sr, a.dtype, a.v.vec);
-          sc[x] = q.x * k.x + q.y * k.y + q.z * k.z + q.w * k.w;
-        }
         n |= sees << x;
+        if (ok) {  // uniform
+          k4[x] = load4(a.k.p, kb + j * a.k.sr, a.dtype, a.k.vec);
+          v4[x] = load4(a.v.p, vb + j * a.v.sr, a.dtype, a.v.vec);
+        }
       }
+#pragma unroll
+      for (int x = 0; x < TB; ++x)
+        sc[x] = n >> x & 1 ? q.x * k4[x].x + q.y * k4[x].y + q.z * k4[x].z + q.w * k4[x].w : 0.f;
       for (int s = quads >> 1; s > 0; s >>= 1)
 #pragma unroll
         for (int x = 0; x < TB; ++x) sc[x] += __shfl_xor(sc[x], s, 64);
+      if (n == 0) continue;
       float mn = m;
 #pragma unroll
-      for (int x = 0; x < TB; ++x) mn = fmaxf(mn, sc[x] *= a.scale_log2);
-      if (mn == -INFINITY && n == 0) continue;
+      for (int x = 0; x < TB; ++x)
+        if (n >> x & 1) mn = fmaxf(mn, sc[x] *= a.scale_log2);
       const float al = m == -INFINITY ? 0.f : exp2f(m - mn);
       l *= al;
       o.x *= al, o.y *= al, o.z *= al, o.w *= al;
@@ -499,18 +933,6 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(PagedAttn a) {
           l += e;
           o.x += e * v4[x].x, o.y += e * v4[x].y, o.z += e * v4[x].z, o.w += e * v4[x].w;
         }
-      m = mn;
-    }
-    // the cached part's units, in their order
-    for (int s = 0; s < un.n; ++s) {
-      const long long row = ((long long)(un.first + s) * a.pool.Hkv + hk) * R + (h % G) * a.nodes + i;
-      const float mu = a.part_ml[row * 2], lu = a.part_ml[row * 2 + 1];
-      const float4 ou = *reinterpret_cast<const float4*>(a.part_o + row * dh + d);
-      if (mu == NO_MAX && lu == 0.f) continue;  // no slot of it is seen
-      const float mn = fmaxf(m, mu);
-      const float al = m == -INFINITY ? 0.f : exp2f(m - mn), e = exp2f(mu - mn);
-      l = l * al + lu * e;
-      o.x = o.x * al + ou.x * e, o.y = o.y * al + ou.y * e, o.z = o.z * al + ou.z * e, o.w = o.w * al + ou.w * e;
       m = mn;
     }
     const float inv = l == 0.f ? 0.f : 1.f / l;  // a row that sees nothing is 0
@@ -545,38 +967,57 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(PagedAttn a) {
 
 }  // namespace
 
-void paged_plan(PagedAttn& a, int max_length) {
-  const int G = a.Hq / a.pool.Hkv, rtiles = (G * a.nodes + 31) / 32;
-  // two workgroups on each of 256 CUs
-  const int streams = a.pool.Hkv * rtiles;
-  a.cut.target = std::max(1, 512 / streams);
-  a.cut.least = 4;  // a tile for each wave
+int paged_plan(PagedAttn& a, int max_length) {
+  const int R = a.Hq / a.pool.Hkv * a.nodes;
   // tiles of a sequence: all, or those that window - 1 slots can touch and the sinks
-  int most = (int)(((long long)max_length + 31) >> 5);
+  long long most = ((long long)max_length + 31) >> 5;
   if (a.cut.window)
-    most = (int)std::min<long long>(most, ((long long)a.cut.window + 30) / 32 + 1 + ((long long)a.cut.sinks + 31) / 32);
+    most = std::min(most, ((long long)a.cut.window + 30) / 32 + 1 + ((long long)a.cut.sinks + 31) / 32);
+  if (most * a.batch > 0x7fffffffLL) return -1;
+  // The wide kernel where a KV head has more than two row tiles and its units
+  // are long: at least 32 tiles for each of the 256 workgroups that then fill
+  // the chip.
+  const int nw = R > 128 ? 8 : 4, wide_blocks = (R + 32 * nw - 1) / (32 * nw);
+  a.wide = R > 64 && a.batch * most * a.pool.Hkv * wide_blocks >= 32 * 256 ? nw : 0;
+  const int streams = a.pool.Hkv * (a.wide ? wide_blocks : (R + 31) / 32);
+  a.cut.target = std::max(1, (a.wide == 8 ? 256 : 512) / streams);
+  a.cut.least = 4;
   // units of a sequence of n tiles: ceil(n / per) with per >= least and >= total / target
   const long long by_len = (long long)a.batch * ((most + a.cut.least - 1) / a.cut.least);
   a.units = (int)std::min<long long>(by_len, (long long)a.cut.target + a.batch);
+  return 0;
 }
 
-size_t paged_workspace_floats(const PagedAttn& a) {
+size_t paged_workspace(PagedAttn& a, void* base) {
   const size_t rows = (size_t)a.units * a.Hq * a.nodes;
-  return rows * (a.pool.dh + 2);
+  a.part_o = static_cast<float*>(base);
+  a.part_ml = a.part_o + rows * a.pool.dh;
+  a.first_unit = reinterpret_cast<int2*>(a.part_ml + rows * 2);
+  return rows * (a.pool.dh + 2) * sizeof(float) + (a.units > 0 ? a.batch * sizeof(int2) : 0);
+}
+
+template <int DH, int QF>
+static void launch_tiles(const PagedAttn& a, dim3 grid, hipStream_t s) {
+  if (a.wide == 8) hipLaunchKernelGGL((paged_wide_kernel<DH, QF == Q_BF16 ? Q_FP8 : QF, 8>), grid, dim3(512), 0, s, a);
+  else if (a.wide) hipLaunchKernelGGL((paged_wide_kernel<DH, QF == Q_BF16 ? Q_FP8 : QF, 4>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((paged_attention_kernel<DH, QF>), grid, dim3(256), 0, s, a);
+}
+
+template <int DH>
+static void launch_form(const PagedAttn& a, dim3 grid, hipStream_t s) {
+  if (a.q_lo.p || a.dtype == PT_F32) launch_tiles<DH, Q_SPLIT>(a, grid, s);
+  else if (a.dtype == PT_F16) launch_tiles<DH, Q_F16>(a, grid, s);
+  else launch_tiles<DH, Q_BF16>(a, grid, s);
 }
 
 hipError_t launch_paged_attention(const PagedAttn& a, hipStream_t s) {
-  const int G = a.Hq / a.pool.Hkv, rtiles = (G * a.nodes + 31) / 32;
-  const bool split = a.dtype == PT_F32 || a.q_lo.p;
+  const int R = a.Hq / a.pool.Hkv * a.nodes, rows = a.wide ? 32 * a.wide : 32;
+  if (a.pool.dh != 64 && a.pool.dh != 128) return hipErrorInvalidValue;
   if (a.units > 0) {
-    const long long streams = ((long long)a.units * a.pool.Hkv + 7) / 8 * 8;
-    if (streams * rtiles > 0x7fffffffLL) return hipErrorInvalidValue;
-    const dim3 grid((unsigned)(streams * rtiles));
-    if (a.pool.dh == 128 && split) hipLaunchKernelGGL((paged_attention_kernel<128, true>), grid, dim3(256), 0, s, a);
-    else if (a.pool.dh == 128) hipLaunchKernelGGL((paged_attention_kernel<128, false>), grid, dim3(256), 0, s, a);
-    else if (a.pool.dh == 64 && split) hipLaunchKernelGGL((paged_attention_kernel<64, true>), grid, dim3(256), 0, s, a);
-    else if (a.pool.dh == 64) hipLaunchKernelGGL((paged_attention_kernel<64, false>), grid, dim3(256), 0, s, a);
-    else return hipErrorInvalidValue;
+    const long long wgs = ((long long)a.units * a.pool.Hkv + 7) / 8 * 8 * ((R + rows - 1) / rows);
+    if (wgs > 0x7fffffffLL) return hipErrorInvalidValue;
+    if (a.pool.dh == 128) launch_form<128>(a, dim3((unsigned)wgs), s);
+    else launch_form<64>(a, dim3((unsigned)wgs), s);
   }
   const dim3 grid(a.batch * a.nodes, (a.Hq * (a.pool.dh / 4) + 255) / 256);
   hipLaunchKernelGGL(paged_combine_kernel, grid, dim3(256), 0, s, a);

@@ -87,8 +87,7 @@ int attention_args(const griffin_attention* g, PagedAttn* out) {
   a.cut.sinks = g->window ? g->sinks : 0;
   rc = paged_table_of(g->pool, g->table, g->table_stride, g->table_cols, g->lengths, g->max_length, &a.tab);
   if (rc != GRIFFIN_OK) return rc;
-  paged_plan(a, a.tab.most);
-  return GRIFFIN_OK;
+  return paged_plan(a, a.tab.most) == 0 ? GRIFFIN_OK : GRIFFIN_ESHAPE;
 }
 
 }  // namespace
@@ -128,7 +127,7 @@ int griffin_paged_append(const griffin_append* g, void* hip_stream) {
 size_t griffin_paged_attention_workspace(const griffin_attention* g) {
   PagedAttn a;
   if (!g || attention_args(g, &a) != GRIFFIN_OK) return 0;
-  return std::max<size_t>(paged_workspace_floats(a) * sizeof(float), 256);
+  return std::max<size_t>(paged_workspace(a, nullptr), 256);
 }
 
 int griffin_paged_attention(const griffin_attention* g, void* workspace, size_t workspace_bytes, void* hip_stream) {
@@ -138,9 +137,9 @@ int griffin_paged_attention(const griffin_attention* g, void* workspace, size_t 
   if (rc != GRIFFIN_OK) return rc;
   for (const griffin_rows* r : {&g->q, &g->k, &g->v, &g->out})
     if (!check_rows(*r, g->dtype)) return GRIFFIN_EINVAL;
-  const size_t floats = paged_workspace_floats(a);
-  if (floats && (!workspace || !aligned(workspace, 16))) return GRIFFIN_EINVAL;
-  if (floats * sizeof(float) > workspace_bytes) return GRIFFIN_ENOMEM;
+  const size_t need = paged_workspace(a, workspace);
+  if (need && (!workspace || !aligned(workspace, 16))) return GRIFFIN_EINVAL;
+  if (need > workspace_bytes) return GRIFFIN_ENOMEM;
   a.counts = g->counts;
   a.anc = g->anc;
   a.q = rows_of(g->q, g->dtype);
@@ -152,8 +151,6 @@ int griffin_paged_attention(const griffin_attention* g, void* workspace, size_t 
   a.orow = o.sr;
   a.oh = o.sh;
   a.out_vec = o.vec;
-  a.part_o = static_cast<float*>(workspace);
-  a.part_ml = a.part_o + (size_t)a.units * a.Hq * a.nodes * a.pool.dh;
   a.status = g->status;
   return launch_paged_attention(a, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? GRIFFIN_OK : GRIFFIN_EHIP;
 }

@@ -323,6 +323,74 @@ def test_long_sequence(G):
     run_case(G, 1, 128, 64, [17001, 40], 1, "f32", hq=2)
 
 
+def on_gpu(pool, table, length, q, k, v, anc, window, sinks):
+    """OP.attention's results in fp64 on the GPU, for one sequence."""
+    n, hq, dh = q.shape
+    s = torch.arange(length, device="cuda")
+    page = pool.k.shape[2] * 32
+    pg, tile, at = table.long()[s // page], s % page // 32, s % 32
+    sees = torch.from_numpy(OP.visible(length, anc, window, sinks)).cuda()
+    o, mag, top = torch.zeros(2, n, hq, dh, dtype=torch.float64, device="cuda").unbind() + (0.0,)
+    group = hq // k.shape[1]
+    for h in range(k.shape[1]):
+        keys = torch.ldexp(pool.k[pg, h, tile, :, at].double().flatten(1), pool.k_exp[pg, h, tile].int()[:, None])
+        vals = torch.ldexp(pool.v[pg, h, tile, :, at].double(), pool.v_exp[pg, h, tile].int()[:, None])
+        keys, vals = torch.cat([keys, k[:, h].double()]), torch.cat([vals, v[:, h].double()])
+        for g in range(h * group, (h + 1) * group):
+            x = q[:, g].double()
+            p = torch.softmax((x @ keys.T * dh**-0.5).masked_fill(~sees, -torch.inf), 1)
+            o[:, g], mag[:, g] = p @ vals, p @ vals.abs()
+            top = max(top, float((x.abs() @ keys.abs().T).max() * dh**-0.5))
+    return o.cpu().numpy(), mag.cpu().numpy(), top
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("dh,hq,heads,nodes,lengths,page,window", [
+    (64, 2, 1, 64, [5, 40000, 0, 33], 128, 0),         # two waves; more tiles than lookups
+    (128, 8, 2, 33, [9000, 31, 64], 64, 0),            # four waves, the last one's rows partly absent
+    (128, 16, 4, 61, [30000, 1], 64, 0),
+    (64, 7, 1, 64, [2049, 640], 32, 0),                # several row blocks
+    (128, 2, 1, 50, [12000, 100, 700], 32, 3000),
+    (64, 4, 1, 61, [12000, 65, 20000], 64, 9000),
+])
+def test_many_rows(G, dtype, dh, hq, heads, nodes, lengths, page, window):
+    """More than two row tiles a key head, under a launch for long sequences:
+    units from one tile to hundreds, full and partial, against fp64 on the GPU."""
+    B, used = len(lengths), [-(-n // page) for n in lengths]
+    pages = sum(used) + 1
+    gen = torch.Generator("cuda").manual_seed(3)
+    pool = G.paged_pool(pages, heads, dh, page)
+    for t in pool[:2]:
+        t.copy_((torch.randn(t.shape, generator=gen, device="cuda") * 40).clamp(-448, 448).to(t.dtype))
+    for t in pool[2:]:
+        t.copy_(torch.randint(-8, -4, t.shape, generator=gen, device="cuda"))
+    # a table of a megaslot, whose unused entries name no page
+    table = torch.full((B, (1 << 20) // page), -1, dtype=torch.int32, device="cuda")
+    perm, at = torch.randperm(pages, generator=gen, device="cuda").int(), 0
+    for b, n in enumerate(used):
+        table[b, :n] = perm[at:at + n]
+        at += n
+    x = torch.randn(B, nodes, hq + 2 * heads, dh, generator=gen, device="cuda")
+    x[:, :, :hq] *= 2
+    q, k, v = x.to(DT[dtype]).split([hq, heads, heads], 2)
+    anc = [tree(nodes, b) for b in range(B)]
+    masks = torch.from_numpy(np.array(anc, dtype=np.uint64).view(np.int64)).cuda()
+    counts = [nodes - 3 * b for b in range(B)]
+    out = torch.full((B, nodes, hq, dh), 7.0, device="cuda", dtype=DT[dtype])
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    args = dict(anc=masks, counts=torch.tensor(counts, dtype=torch.int32, device="cuda"), window=window, sinks=37 if window else 0)
+    lens = torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    G.paged_attention(pool, table, lens, q, k, v, out=out, status=status, **args)
+    assert status.item() == 0
+    again = torch.full_like(out, 7.0)
+    assert torch.equal(G.paged_attention(pool, table, lens, q, k, v, out=again, **args), out)
+    got = out.double().cpu().numpy()
+    for b, c in enumerate(counts):
+        o, mag, top = on_gpu(pool, table[b], lengths[b], q[b, :c], k[b, :c], v[b, :c], anc[b][:c], window, args["sinks"])
+        check(got[b, :c], o, mag, top, dh, lengths[b] + c, dtype)
+        assert (got[b, c:] == 7.0).all()
+
+
 @pytest.mark.parametrize("window,sinks", [(1, 0), (1, 3), (2, 0), (33, 0), (64, 4), (100, 40), (100, 300), (5000, 4), (7, 33)])
 @pytest.mark.parametrize("nodes,dtype", [(1, "bf16"), (9, "f32"), (64, "f16")])
 def test_windows(G, window, sinks, nodes, dtype):
