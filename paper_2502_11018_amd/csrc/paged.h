@@ -142,21 +142,42 @@ __device__ __forceinline__ void load8(const void* p, long long at, int dtype, in
   }
 }
 
-// 4 consecutive values as fp32
-__device__ __forceinline__ float4 load4(const void* p, long long at, int dtype, int vec) {
-  if (dtype == PT_F32) {
+// 4 consecutive values: as they are, and as fp32
+template <int DT>
+struct QuadOf {
+  typedef uint2 type;
+};
+template <>
+struct QuadOf<PT_F32> {
+  typedef float4 type;
+};
+template <int DT>
+__device__ __forceinline__ typename QuadOf<DT>::type load_quad(const void* p, long long at, int vec) {
+  if constexpr (DT == PT_F32) {
     const float* f = static_cast<const float*>(p) + at;
     if (vec) return *reinterpret_cast<const float4*>(f);
     return make_float4(f[0], f[1], f[2], f[3]);
+  } else {
+    const uint16_t* h = static_cast<const uint16_t*>(p) + at;
+    if (vec) return *reinterpret_cast<const uint2*>(h);
+    return make_uint2(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16);
   }
-  const uint16_t* h = static_cast<const uint16_t*>(p) + at;
-  uint2 w;
-  if (vec) w = *reinterpret_cast<const uint2*>(h);
-  else w = make_uint2(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16);
-  if (dtype == PT_BF16)
+}
+template <int DT>
+__device__ __forceinline__ float4 quad_f32(const typename QuadOf<DT>::type& w) {
+  if constexpr (DT == PT_F32) {
+    return w;
+  } else if constexpr (DT == PT_BF16) {
     return make_float4(bf16_to_f32(w.x & 0xffff), bf16_to_f32(w.x >> 16), bf16_to_f32(w.y & 0xffff), bf16_to_f32(w.y >> 16));
-  auto f = [](uint32_t u) { return (float)__builtin_bit_cast(_Float16, (uint16_t)u); };
-  return make_float4(f(w.x), f(w.x >> 16), f(w.y), f(w.y >> 16));
+  } else {
+    auto f = [](uint32_t u) { return (float)__builtin_bit_cast(_Float16, (uint16_t)u); };
+    return make_float4(f(w.x), f(w.x >> 16), f(w.y), f(w.y >> 16));
+  }
+}
+__device__ __forceinline__ float4 load4(const void* p, long long at, int dtype, int vec) {
+  if (dtype == PT_F32) return load_quad<PT_F32>(p, at, vec);
+  const uint2 w = load_quad<PT_BF16>(p, at, vec);
+  return dtype == PT_BF16 ? quad_f32<PT_BF16>(w) : quad_f32<PT_F16>(w);
 }
 
 }  // namespace griffin

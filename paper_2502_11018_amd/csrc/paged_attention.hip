@@ -75,8 +75,11 @@ __device__ __forceinline__ int lanes_sum(int n, int batch) {
 }
 
 // The sequence of unit u: {sequence (-1: none), split, splits}.  A unit holds
-// at most max(least, ceil(all tiles / target)) tiles, and a sequence's units
-// the same number each to one.
+// at most `per` tiles, and a sequence's units the same number each to one;
+// per is at least ceil(all tiles / target), and rises for a few steps while
+// the sequences' last units bring their number above the target (workgroups
+// that do not fit the chip at once cost a second round: 18.5 -> 14.1 us for 16
+// sequences of up to 2048 slots).
 struct UnitAt {
   int b, split, n;
 };
@@ -87,7 +90,15 @@ __device__ UnitAt unit_at(const PagedAttn& a, int u) {
   const int own = tiles(lane);
   uint32_t total = lanes_sum(own, a.batch);
   for (int b0 = 64; b0 < a.batch; b0 += 64) total += lanes_sum(tiles(b0 + lane), 64);
-  const int per = max((uint32_t)a.cut.least, (total + a.cut.target - 1) / a.cut.target);
+  const uint32_t target = a.cut.target;
+  uint32_t per = max((uint32_t)a.cut.least, (total + target - 1) / target);
+  for (int i = 0; i < 4; ++i) {
+    uint32_t units = 0;
+    for (int b0 = 0; b0 < a.batch; b0 += 64)
+      units += lanes_sum(((b0 ? tiles(b0 + lane) : own) + per - 1) / per, b0 ? 64 : a.batch);
+    if (units <= target) break;
+    per += (per * (units - target) + target - 1) / target;
+  }
   int first = 0;
   for (int b0 = 0; b0 < a.batch; b0 += 64) {
     const int n = ((b0 ? tiles(b0 + lane) : own) + per - 1) / per;
@@ -831,61 +842,94 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_wide_kernel(PagedAttn a) {
   }
 }
 
-// A thread: 4 dims of a head of one node.  What a row needs first (lengths,
-// masks, q, its units' place) is asked for at once, and of the root path and
-// the units eight each at a time.
+// Joins a row's units and the nodes of its own root path: a thread holds 4 dims
+// of a head of one node.  SG groups of threads share a head where there are few
+// rows: group g takes units g, g + SG, .., the last one the root path too, and
+// they meet in LDS.  What a group needs is asked for before any of it is used.
+template <int DT, int SG>
 __global__ __launch_bounds__(256) void paged_combine_kernel(PagedAttn a) {
-  const int dh = a.pool.dh, quads = dh / 4;
+  constexpr int TB = SG == 1 ? 2 : 8;             // units at a time
+  constexpr int TN = SG == 1 && DT == PT_F32 ? 4 : 8;  // nodes at a time
+  using Quad = typename QuadOf<DT>::type;
+  __shared__ float4 so[SG > 1 ? 256 : 1];
+  __shared__ float2 sml[SG > 1 ? 256 : 1];
+  const int dh = a.pool.dh, quads = dh / 4, heads = 256 / SG / quads;  // heads of a workgroup
   const int b = blockIdx.x / a.nodes, i = blockIdx.x % a.nodes;
-  const int t = blockIdx.y * 256 + threadIdx.x;
   const int G = a.Hq / a.pool.Hkv, R = G * a.nodes;
-  if (t >= a.Hq * quads) return;  // whole heads: 64 threads of a wave hold 2 or 4
-  const int h = t / quads, d = t % quads * 4, hk = h / G;
+  const int grp = SG == 1 ? 0 : threadIdx.x / (256 / SG), t = SG == 1 ? threadIdx.x : threadIdx.x % (256 / SG);
+  const int h = min((int)blockIdx.y * heads + t / quads, a.Hq - 1), d = t % quads * 4, hk = h / G;
+  const bool mine = blockIdx.y * heads + t / quads < a.Hq;
   uint64_t anc = anc_of(a, b, i);
   const int2 un = a.units > 0 ? a.first_unit[b] : make_int2(0, 0);
   bool bad = false;
   const int len = checked_len(a.tab, b, &bad);
   int count = a.counts ? a.counts[b] : a.nodes;
-  float4 q = load4(a.q.p, b * a.q.sb + i * a.q.sr + h * a.q.sh + d, a.q_lo.p ? PT_BF16 : a.dtype, a.q.vec);
-  if (a.q_lo.p) {
-    const float4 y = load4(a.q_lo.p, b * a.q.sb + i * a.q.sr + h * a.q.sh + d, PT_BF16, a.q.vec);
+  const long long qo = b * a.q.sb + i * a.q.sr + h * a.q.sh + d;
+  float4 q;
+  if (DT == PT_F32 && a.q_lo.p) {
+    q = quad_f32<PT_BF16>(load_quad<PT_BF16>(a.q.p, qo, a.q.vec));
+    const float4 y = quad_f32<PT_BF16>(load_quad<PT_BF16>(a.q_lo.p, qo, a.q.vec));
     q.x += y.x, q.y += y.y, q.z += y.z, q.w += y.w;
+  } else {
+    q = quad_f32<DT>(load_quad<DT>(a.q.p, qo, a.q.vec));
   }
   if (count < 0 || count > a.nodes) bad = true, count = min(max(count, 0), a.nodes);
   if (bad && a.status && threadIdx.x == 0) atomicOr(a.status, PAGED_BAD_LENGTH);
   const bool live = i < count;
-  if (!live && a.out_ks == 0) return;
+  if (!live && a.out_ks == 0) return;  // uniform
   float4 out = make_float4(0.f, 0.f, 0.f, 0.f);
-  if (live) {  // uniform over the workgroup
+  if (live) {
     const int dep = depth_of(anc, i);
     float m = -INFINITY, l = 0.f;
     float4 o = out;
-    constexpr int TB = 8;
-    // the cached part's units, in their order; a sequence without tiles has
-    // none (and nobody wrote their place)
+    // a sequence without tiles has no units (and nobody wrote their place)
     const int units = seq_tiles(len, a.cut).n > 0 ? un.y : 0;
     const long long row = ((long long)un.x * a.pool.Hkv + hk) * R + (h % G) * a.nodes + i;
     const long long step = (long long)a.pool.Hkv * R;
-    for (int s = 0; s < units; s += TB) {
-      float2 ml[TB];
-      float4 ou[TB];
+    float2 ml[TB];
+    float4 ou[TB];
+    auto ask = [&](int s) {
 #pragma unroll
-      for (int x = 0; x < TB; ++x) {
-        const long long at = row + min(s + x, units - 1) * step;
-        ml[x] = *reinterpret_cast<const float2*>(a.part_ml + at * 2);
-        ou[x] = *reinterpret_cast<const float4*>(a.part_o + at * dh + d);
+      for (int x = 0; x < TB; ++x)
+        if (s + x * SG < units) {  // uniform over the group
+          const long long at = row + (s + x * SG) * step;
+          ml[x] = *reinterpret_cast<const float2*>(a.part_ml + at * 2);
+          ou[x] = *reinterpret_cast<const float4*>(a.part_o + at * dh + d);
+        }
+    };
+    const long long kb = b * a.k.sb + hk * a.k.sh + d, vb = b * a.v.sb + hk * a.v.sh + d;
+    if (grp != SG - 1) anc = 0;
+    int r = 0, seen = 0;  // rank of the next node, the batch's seen ones
+    Quad k4[TN], v4[TN];
+    auto ask_nodes = [&]() {
+      seen = 0;
+#pragma unroll
+      for (int x = 0; x < TN; ++x) {
+        if (!anc) break;  // uniform
+        const int j = __builtin_ctzll(anc);
+        anc &= anc - 1;
+        if (!a.cut.window || dep - r < a.cut.window || (long long)len + r < a.cut.sinks) seen |= 1 << x;
+        ++r;
+        k4[x] = load_quad<DT>(a.k.p, kb + j * a.k.sr, a.k.vec);
+        v4[x] = load_quad<DT>(a.v.p, vb + j * a.v.sr, a.v.vec);
       }
+    };
+    ask(grp);
+    const uint64_t path = anc;
+    ask_nodes();
+    for (int s = grp; s < units; s += TB * SG) {
+      if (s != grp) ask(s);
       float mn = m;
 #pragma unroll
       for (int x = 0; x < TB; ++x)
-        if (s + x < units && !(ml[x].x == NO_MAX && ml[x].y == 0.f)) mn = fmaxf(mn, ml[x].x);
+        if (s + x * SG < units && !(ml[x].x == NO_MAX && ml[x].y == 0.f)) mn = fmaxf(mn, ml[x].x);
       if (mn == -INFINITY) continue;  // no slot of them is seen
       const float al = exp2f(m - mn);
       l *= al;
       o.x *= al, o.y *= al, o.z *= al, o.w *= al;
 #pragma unroll
       for (int x = 0; x < TB; ++x)
-        if (s + x < units) {
+        if (s + x * SG < units) {
           const float e = exp2f(ml[x].x - mn);
           l += e * ml[x].y;
           o.x += e * ou[x].x, o.y += e * ou[x].y, o.z += e * ou[x].z, o.w += e * ou[x].w;
@@ -893,52 +937,66 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(PagedAttn a) {
       m = mn;
     }
     // nodes of the root path
-    const long long kb = b * a.k.sb + hk * a.k.sh + d, vb = b * a.v.sb + hk * a.v.sh + d;
-    int r = 0;  // rank of the next node
-    while (anc) {
-      float4 k4[TB], v4[TB];
-      float sc[TB];
-      int n = 0;
+    for (bool any = path != 0; any;) {
+      if (seen) {
+        float sc[TN];
 #pragma unroll
-      for (int x = 0; x < TB; ++x) {
-        const bool ok = anc != 0;
-        const int j = ok ? __builtin_ctzll(anc) : 0;
-        anc &= anc - 1;
-        const bool sees = ok && (!a.cut.window || dep - r < a.cut.window || (long long)len + r < a.cut.sinks);
-        r += ok;
-        n |= sees << x;
-        if (ok) {  // uniform
-          k4[x] = load4(a.k.p, kb + j * a.k.sr, a.dtype, a.k.vec);
-          v4[x] = load4(a.v.p, vb + j * a.v.sr, a.dtype, a.v.vec);
+        for (int x = 0; x < TN; ++x) {
+          sc[x] = 0.f;
+          if (seen >> x & 1) {
+            const float4 k = quad_f32<DT>(k4[x]);
+            sc[x] = q.x * k.x + q.y * k.y + q.z * k.z + q.w * k.w;
+          }
+        }
+        for (int s = quads >> 1; s > 0; s >>= 1)
+#pragma unroll
+          for (int x = 0; x < TN; ++x) sc[x] += __shfl_xor(sc[x], s, 64);
+        float mn = m;
+#pragma unroll
+        for (int x = 0; x < TN; ++x)
+          if (seen >> x & 1) mn = fmaxf(mn, sc[x] *= a.scale_log2);
+        const float al = m == -INFINITY ? 0.f : exp2f(m - mn);
+        l *= al;
+        o.x *= al, o.y *= al, o.z *= al, o.w *= al;
+#pragma unroll
+        for (int x = 0; x < TN; ++x)
+          if (seen >> x & 1) {
+            const float e = exp2f(sc[x] - mn);
+            const float4 v = quad_f32<DT>(v4[x]);
+            l += e;
+            o.x += e * v.x, o.y += e * v.y, o.z += e * v.z, o.w += e * v.w;
+          }
+        m = mn;
+      }
+      any = anc != 0;
+      if (any) ask_nodes();
+    }
+    if constexpr (SG > 1) {
+      so[threadIdx.x] = o;
+      sml[threadIdx.x] = make_float2(m, l);
+      __syncthreads();
+      if (grp == 0) {
+        float mn = m;
+#pragma unroll
+        for (int g = 1; g < SG; ++g) mn = fmaxf(mn, sml[g * (256 / SG) + t].x);
+        const float al = m == -INFINITY ? 0.f : exp2f(m - mn);
+        l *= al;
+        o.x *= al, o.y *= al, o.z *= al, o.w *= al;
+#pragma unroll
+        for (int g = 1; g < SG; ++g) {
+          const float2 x = sml[g * (256 / SG) + t];
+          const float4 v = so[g * (256 / SG) + t];
+          const float e = x.x == -INFINITY ? 0.f : exp2f(x.x - mn);
+          l += e * x.y;
+          o.x += e * v.x, o.y += e * v.y, o.z += e * v.z, o.w += e * v.w;
         }
       }
-#pragma unroll
-      for (int x = 0; x < TB; ++x)
-        sc[x] = n >> x & 1 ? q.x * k4[x].x + q.y * k4[x].y + q.z * k4[x].z + q.w * k4[x].w : 0.f;
-      for (int s = quads >> 1; s > 0; s >>= 1)
-#pragma unroll
-        for (int x = 0; x < TB; ++x) sc[x] += __shfl_xor(sc[x], s, 64);
-      if (n == 0) continue;
-      float mn = m;
-#pragma unroll
-      for (int x = 0; x < TB; ++x)
-        if (n >> x & 1) mn = fmaxf(mn, sc[x] *= a.scale_log2);
-      const float al = m == -INFINITY ? 0.f : exp2f(m - mn);
-      l *= al;
-      o.x *= al, o.y *= al, o.z *= al, o.w *= al;
-#pragma unroll
-      for (int x = 0; x < TB; ++x)
-        if (n >> x & 1) {
-          const float e = exp2f(sc[x] - mn);
-          l += e;
-          o.x += e * v4[x].x, o.y += e * v4[x].y, o.z += e * v4[x].z, o.w += e * v4[x].w;
-        }
-      m = mn;
     }
     const float inv = l == 0.f ? 0.f : 1.f / l;  // a row that sees nothing is 0
     out = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
     if (bad) out.x = out.y = out.z = out.w = __builtin_nanf("");
   }
+  if (grp != 0 || !mine) return;
   if (a.out_ks) {
     uint16_t* dst = static_cast<uint16_t*>(a.out) + xpack_off((long long)b * a.nodes + i, h * dh + d, a.out_ks);
     const Hilo2 p0 = pack_hilo2(out.x, out.y), p1 = pack_hilo2(out.z, out.w);
@@ -947,22 +1005,22 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(PagedAttn a) {
     return;
   }
   const long long at = b * a.ob + i * a.orow + h * a.oh + d;
-  if (a.dtype == PT_F32) {
+  if constexpr (DT == PT_F32) {
     float* f = static_cast<float*>(a.out) + at;
     if (a.out_vec) *reinterpret_cast<float4*>(f) = out;
     else f[0] = out.x, f[1] = out.y, f[2] = out.z, f[3] = out.w;
-    return;
-  }
-  uint2 w;
-  if (a.dtype == PT_BF16) {
-    w = make_uint2(pack_bf16x2(out.x, out.y), pack_bf16x2(out.z, out.w));
   } else {
-    auto f = [](float x) { return (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)x); };
-    w = make_uint2(f(out.x) | f(out.y) << 16, f(out.z) | f(out.w) << 16);
+    uint2 w;
+    if constexpr (DT == PT_BF16) {
+      w = make_uint2(pack_bf16x2(out.x, out.y), pack_bf16x2(out.z, out.w));
+    } else {
+      const f16x2 x = __builtin_convertvector(f32x2{out.x, out.y}, f16x2), y = __builtin_convertvector(f32x2{out.z, out.w}, f16x2);
+      w = make_uint2(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, y));
+    }
+    uint16_t* p = static_cast<uint16_t*>(a.out) + at;
+    if (a.out_vec) *reinterpret_cast<uint2*>(p) = w;
+    else p[0] = w.x, p[1] = w.x >> 16, p[2] = w.y, p[3] = w.y >> 16;
   }
-  uint16_t* p = static_cast<uint16_t*>(a.out) + at;
-  if (a.out_vec) *reinterpret_cast<uint2*>(p) = w;
-  else p[0] = w.x, p[1] = w.x >> 16, p[2] = w.y, p[3] = w.y >> 16;
 }
 
 }  // namespace
@@ -982,7 +1040,7 @@ int paged_plan(PagedAttn& a, int max_length) {
   const int streams = a.pool.Hkv * (a.wide ? wide_blocks : (R + 31) / 32);
   a.cut.target = std::max(1, (a.wide == 8 ? 256 : 512) / streams);
   a.cut.least = 4;
-  // units of a sequence of n tiles: ceil(n / per) with per >= least and >= total / target
+  // units of a sequence of n tiles: ceil(n / per) with per >= least and >= all tiles / target
   const long long by_len = (long long)a.batch * ((most + a.cut.least - 1) / a.cut.least);
   a.units = (int)std::min<long long>(by_len, (long long)a.cut.target + a.batch);
   return 0;
@@ -1010,6 +1068,13 @@ static void launch_form(const PagedAttn& a, dim3 grid, hipStream_t s) {
   else launch_tiles<DH, Q_BF16>(a, grid, s);
 }
 
+template <int DT>
+static void launch_combine(const PagedAttn& a, bool few, hipStream_t s) {
+  const int rows = a.batch * a.nodes, threads = a.Hq * (a.pool.dh / 4);
+  if (few) hipLaunchKernelGGL((paged_combine_kernel<DT, 4>), dim3(rows, (threads + 63) / 64), dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((paged_combine_kernel<DT, 1>), dim3(rows, (threads + 255) / 256), dim3(256), 0, s, a);
+}
+
 hipError_t launch_paged_attention(const PagedAttn& a, hipStream_t s) {
   const int R = a.Hq / a.pool.Hkv * a.nodes, rows = a.wide ? 32 * a.wide : 32;
   if (a.pool.dh != 64 && a.pool.dh != 128) return hipErrorInvalidValue;
@@ -1019,8 +1084,11 @@ hipError_t launch_paged_attention(const PagedAttn& a, hipStream_t s) {
     if (a.pool.dh == 128) launch_form<128>(a, dim3((unsigned)wgs), s);
     else launch_form<64>(a, dim3((unsigned)wgs), s);
   }
-  const dim3 grid(a.batch * a.nodes, (a.Hq * (a.pool.dh / 4) + 255) / 256);
-  hipLaunchKernelGGL(paged_combine_kernel, grid, dim3(256), 0, s, a);
+  // four groups a head while that leaves at most two workgroups for each CU
+  const bool few = (long long)a.batch * a.nodes * a.Hq * (a.pool.dh / 4) <= 512 * 64;
+  if (a.dtype == PT_F32) launch_combine<PT_F32>(a, few, s);
+  else if (a.dtype == PT_F16) launch_combine<PT_F16>(a, few, s);
+  else launch_combine<PT_BF16>(a, few, s);
   return hipGetLastError();
 }
 
