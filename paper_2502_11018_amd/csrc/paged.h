@@ -73,8 +73,9 @@ hipError_t launch_paged_append(PagedAppend a, hipStream_t s);
 // sequence after sequence.
 struct PagedCut {
   int window, sinks;
-  int target;  // units wanted in all
+  int target;  // units wanted in all: workgroups that fit the chip at once
   int least;   // tiles per unit at least
+  int full;    // tiles per unit from which on all of the target is used
 };
 
 struct PagedAttn {

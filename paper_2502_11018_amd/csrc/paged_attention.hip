@@ -90,7 +90,9 @@ __device__ UnitAt unit_at(const PagedAttn& a, int u) {
   const int own = tiles(lane);
   uint32_t total = lanes_sum(own, a.batch);
   for (int b0 = 64; b0 < a.batch; b0 += 64) total += lanes_sum(tiles(b0 + lane), 64);
-  const uint32_t target = a.cut.target;
+  // half the target while units are short: a unit's start and join cost more
+  // than what the second workgroup of a CU hides
+  const uint32_t target = total >= (uint32_t)a.cut.target * a.cut.full ? a.cut.target : (a.cut.target + 1) / 2;
   uint32_t per = max((uint32_t)a.cut.least, (total + target - 1) / target);
   for (int i = 0; i < 4; ++i) {
     uint32_t units = 0;
@@ -488,10 +490,11 @@ __device__ __forceinline__ void load_vals(const PagedAttn& a, long long at, int 
   for (int x = 0; x < DH / 32; ++x) v.r[x] = *reinterpret_cast<const u32x4*>(p + 1024 * x);
 }
 
-// A row tile's output to LDS: row r at buf[r * DH ..], its 16-byte chunk c at
+// The first `rows` rows of a row tile's output to LDS: row r at buf[r * DH ..], its 16-byte chunk c at
 // c ^ (r & 7) (conflict-free here and where rows are read).
 template <int DH>
-__device__ __forceinline__ void put_rows(const State<DH>& st, int col, int hh, float* buf) {
+__device__ __forceinline__ void put_rows(const State<DH>& st, int col, int hh, int rows, float* buf) {
+  if (col >= rows) return;
   const float fe = pow2i(st.E);
 #pragma unroll
   for (int d = 0; d < DH / 32; ++d)
@@ -586,7 +589,7 @@ __global__ __launch_bounds__(256, 2) void paged_attention_kernel(PagedAttn a) {
   }
   float l = st.l + __shfl_xor(st.l, 32, 64);
   if (__any(p.bad)) l = __builtin_nanf("");  // a tile that is not there: the rows become NaN
-  put_rows<DH>(st, col, hh, so[w]);
+  put_rows<DH>(st, col, hh, R - p.rb * 32, so[w]);
   if (hh == 0) sm[w][col] = st.m, sl[w][col] = l;
   __syncthreads();
   constexpr int CH = DH / 4;
@@ -594,7 +597,7 @@ __global__ __launch_bounds__(256, 2) void paged_attention_kernel(PagedAttn a) {
   const int live = min(32, R - p.rb * 32);
   for (int i = threadIdx.x; i < live * CH; i += 256) {
     const int r = i / CH, c = i % CH;
-    if ((p.rb * 32 + r) % a.nodes >= count) continue;  // an absent node
+    if (count < a.nodes && (p.rb * 32 + r) % a.nodes >= count) continue;  // an absent node
     float M = sm[0][r];
 #pragma unroll
     for (int x = 1; x < NW; ++x) M = fmaxf(M, sm[x][r]);
@@ -830,8 +833,8 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_wide_kernel(PagedAttn a) {
   __syncthreads();  // every wave has left the ring
   float l = st.l + __shfl_xor(st.l, 32, 64);
   if (hurt) l = __builtin_nanf("");
-  put_rows<DH>(st, col, hh, buf);
-  auto live = [&](int r) { return row0 + r < R && (row0 + r) % a.nodes < count; };
+  put_rows<DH>(st, col, hh, R - row0, buf);
+  auto live = [&](int r) { return row0 + r < R && (count >= a.nodes || (row0 + r) % a.nodes < count); };
   if (hh == 0 && live(col)) *reinterpret_cast<float2*>(a.part_ml + (prow + col) * 2) = make_float2(st.m, l);
 #pragma unroll 4
   for (int n = 0; n < 32 / RPI; ++n) {
@@ -1039,7 +1042,8 @@ int paged_plan(PagedAttn& a, int max_length) {
   a.wide = R > 64 && a.batch * most * a.pool.Hkv * wide_blocks >= 32 * 256 ? nw : 0;
   const int streams = a.pool.Hkv * (a.wide ? wide_blocks : (R + 31) / 32);
   a.cut.target = std::max(1, (a.wide == 8 ? 256 : 512) / streams);
-  a.cut.least = 4;
+  a.cut.least = 8;
+  a.cut.full = a.wide ? 0 : 32;
   // units of a sequence of n tiles: ceil(n / per) with per >= least and >= all tiles / target
   const long long by_len = (long long)a.batch * ((most + a.cut.least - 1) / a.cut.least);
   a.units = (int)std::min<long long>(by_len, (long long)a.cut.target + a.batch);

@@ -131,7 +131,7 @@ def test_attention_wants_its_workspace():
     N = _lib()
     args = attention_args(most=100)
     need = N.lib.griffin_paged_attention_workspace(args)
-    # one unit of at most four tiles of 32 slots: 8 rows of 128 outputs and 2 sums, and the unit's place
+    # one unit of at most eight tiles of 32 slots: 8 rows of 128 outputs and 2 sums, and the unit's place
     assert need == 8 * 130 * 4 + 8
     assert N.lib.griffin_paged_attention(args, 256, need - 1, None) == N.CODES["GRIFFIN_ENOMEM"]
     assert N.lib.griffin_paged_attention(args, 0, need, None) == N.CODES["GRIFFIN_EINVAL"]
