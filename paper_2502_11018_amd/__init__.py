@@ -19,7 +19,8 @@ def __getattr__(name):
     if name in _EXPORTS:
         import importlib
         mod = importlib.import_module(f".{_EXPORTS[name]}", __name__)
-        return getattr(mod, name)
+        globals()[name] = getattr(mod, name)  # later lookups do not come here
+        return globals()[name]
     raise AttributeError(name)
 
 

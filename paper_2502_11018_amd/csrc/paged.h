@@ -175,10 +175,4 @@ __device__ __forceinline__ float4 quad_f32(const typename QuadOf<DT>::type& w) {
     return make_float4(f(w.x), f(w.x >> 16), f(w.y), f(w.y >> 16));
   }
 }
-__device__ __forceinline__ float4 load4(const void* p, long long at, int dtype, int vec) {
-  if (dtype == PT_F32) return load_quad<PT_F32>(p, at, vec);
-  const uint2 w = load_quad<PT_BF16>(p, at, vec);
-  return dtype == PT_BF16 ? quad_f32<PT_BF16>(w) : quad_f32<PT_F16>(w);
-}
-
 }  // namespace griffin

@@ -15,6 +15,7 @@
 // Later slots of the tile keep their bytes.
 
 #include <algorithm>
+#include <type_traits>
 
 #include "paged.h"
 
@@ -34,24 +35,35 @@ __device__ __forceinline__ float finite_abs(float x) {
   return a <= 3.402823466e38f ? a : 0.f;
 }
 
-// 4 values to e4m3, the first in the low byte
+// The conversion to e4m3 turns what is above 448 into a NaN.  Finite numbers
+// are within it by their tile's exponent; infinities are clamped where a tile
+// has any (a NaN passes).
+template <bool INF>
 __device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d) {
-  // the conversion turns what is above 448 into a NaN: clamp, which a NaN passes
-  auto sat = [](float x) { return x > 448.f ? 448.f : x < -448.f ? -448.f : x; };
+  auto sat = [](float x) { return !INF ? x : x > 448.f ? 448.f : x < -448.f ? -448.f : x; };
   const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(sat(a), sat(b), 0, false);
   return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(sat(c), sat(d), lo, true);
 }
 
 __device__ __forceinline__ uint32_t rescale_e4m3(uint32_t w, float f) {
-  return pack_e4m3(__builtin_amdgcn_cvt_f32_fp8(w, 0) * f, __builtin_amdgcn_cvt_f32_fp8(w, 1) * f,
-                   __builtin_amdgcn_cvt_f32_fp8(w, 2) * f, __builtin_amdgcn_cvt_f32_fp8(w, 3) * f);
+  return pack_e4m3<false>(__builtin_amdgcn_cvt_f32_fp8(w, 0) * f, __builtin_amdgcn_cvt_f32_fp8(w, 1) * f,
+                          __builtin_amdgcn_cvt_f32_fp8(w, 2) * f, __builtin_amdgcn_cvt_f32_fp8(w, 3) * f);
 }
 
-// Threads: DH * 2, (slot, j) = (t % 32, t / 32): the key's dims 8 j .. and
-// DH / 2 + 8 j .. of a slot, and of the values 4 slots x 4 dims.
-template <int DH>
+// What a thread reads of one head: of a slot's key the dims 8 j .. and dh / 2 +
+// 8 j .., and of the values 4 slots x 4 dims.
+template <int DT>
+struct HeadRows {
+  typedef typename QuadOf<DT>::type Quad;
+  Quad k[4], v[4];
+};
+
+// Threads: DH * 2, (slot, j) = (t % 32, t / 32) for the keys, (slots 4 vg ..,
+// dims 4 vd ..) = (t % 8, t / 8) for the values.
+template <int DH, int DT>
 __global__ __launch_bounds__(DH * 2) void paged_append_kernel(PagedAppend a) {
   constexpr int NT = DH * 2, NW = NT / 64, HALF = DH / 2;
+  typedef typename QuadOf<DT>::type Quad;
   __shared__ float red[2][2][NW];
   const int t = threadIdx.x;
   const int groups = (a.pool.Hkv + a.heads_per_wg - 1) / a.heads_per_wg;
@@ -74,12 +86,7 @@ __global__ __launch_bounds__(DH * 2) void paged_append_kernel(PagedAppend a) {
   const int s0 = tile * 32;
   if (n == 0 || s0 >= len + n) return;
   const int page = a.tab.pages[(long long)b * a.tab.stride + tile / a.pool.tpp];
-  if (page < 0 || page >= a.pool.n_pages) {
-    if (a.status && t == 0) atomicOr(a.status, PAGED_BAD_PAGE);
-    return;
-  }
   const int h0 = g * a.heads_per_wg, h1 = min(h0 + a.heads_per_wg, a.pool.Hkv);
-  const long long tile0 = layer * a.pool_layer + (long long)page * a.pool.Hkv * a.pool.tpp + tile % a.pool.tpp;
 
   // source row of a slot: -1 none (an earlier or a later slot), -2 out of range
   auto row_of = [&](int slot) -> int {
@@ -92,12 +99,31 @@ __global__ __launch_bounds__(DH * 2) void paged_append_kernel(PagedAppend a) {
   };
   const int slot = s0 + t % 32, j = t / 32;
   const int krow = row_of(slot);
-  // values: slots 4 vg .. + 3, dims 4 vd .. + 3
   const int vg = t % 8, vd = t / 8;
   int vrow[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) vrow[i] = row_of(s0 + 4 * vg + i);
+  const long long kb = layer * a.rows_layer + b * a.k.sb + 8 * j, vb = layer * a.rows_layer + b * a.v.sb + 4 * vd;
+  auto read = [&](int h, HeadRows<DT>& r) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r.k[i] = r.v[i] = Quad{};
+    if (krow >= 0) {
+      const long long at = kb + krow * a.k.sr + h * a.k.sh;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) r.k[i] = load_quad<DT>(a.k.p, at + (i / 2) * HALF + 4 * (i % 2), a.k.vec);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (vrow[i] >= 0) r.v[i] = load_quad<DT>(a.v.p, vb + vrow[i] * a.v.sr + h * a.v.sh, a.v.vec);
+  };
+  HeadRows<DT> now, next;
+  read(h0, now);  // asked for before the page is known
   if (a.status && krow == -2) atomicOr(a.status, PAGED_BAD_ROW);
+  if (page < 0 || page >= a.pool.n_pages) {  // uniform
+    if (a.status && t == 0) atomicOr(a.status, PAGED_BAD_PAGE);
+    return;
+  }
+  const long long tile0 = layer * a.pool_layer + (long long)page * a.pool.Hkv * a.pool.tpp + tile % a.pool.tpp;
   const bool held = s0 < len;  // the tile has earlier slots
 
   float cs[8], sn[8];
@@ -109,24 +135,19 @@ __global__ __launch_bounds__(DH * 2) void paged_append_kernel(PagedAppend a) {
       sincospif(2.f * (float)rev, &sn[i], &cs[i]);
     }
   }
-  const long long kb = layer * a.rows_layer + b * a.k.sb, vb = layer * a.rows_layer + b * a.v.sb;
   for (int h = h0; h < h1; ++h) {
-    float x[8], y[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = y[i] = 0.f;
-    if (krow >= 0) {
-      const long long at = kb + krow * a.k.sr + h * a.k.sh + 8 * j;
-      load8(a.k.p, at, a.dtype, a.k.vec, x);
-      load8(a.k.p, at + HALF, a.dtype, a.k.vec, y);
-    }
-    float4 z[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      z[i] = vrow[i] >= 0 ? load4(a.v.p, vb + vrow[i] * a.v.sr + h * a.v.sh + 4 * vd, a.dtype, a.v.vec)
-                          : make_float4(0.f, 0.f, 0.f, 0.f);
+    if (h + 1 < h1) read(h + 1, next);
     const long long ti = tile0 + (long long)h * a.pool.tpp;
     int ke = PAGED_E_MIN, ve = PAGED_E_MIN;
     if (held) ke = a.pool.ke[ti], ve = a.pool.ve[ti];
+    float x[8], y[8], z[4][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float4 k = quad_f32<DT>(now.k[i]), v = quad_f32<DT>(now.v[i]);
+      float* d = i < 2 ? x + 4 * i : y + 4 * (i - 2);
+      d[0] = k.x, d[1] = k.y, d[2] = k.z, d[3] = k.w;
+      z[i][0] = v.x, z[i][1] = v.y, z[i][2] = v.z, z[i][3] = v.w;
+    }
     if (a.rotate) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
@@ -137,79 +158,99 @@ __global__ __launch_bounds__(DH * 2) void paged_append_kernel(PagedAppend a) {
     }
     float mk = 0.f, mv = 0.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) mk = fmaxf(mk, fmaxf(finite_abs(x[i]), finite_abs(y[i])));
+    for (int i = 0; i < 8; ++i) mk = fmaxf(mk, fmaxf(fabsf(x[i]), fabsf(y[i])));
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      mv = fmaxf(mv, fmaxf(fmaxf(finite_abs(z[i].x), finite_abs(z[i].y)), fmaxf(finite_abs(z[i].z), finite_abs(z[i].w))));
-    mk = wave_max(mk), mv = wave_max(mv);
-    float(&rd)[2][NW] = red[h & 1];  // two sets: the next head's maxima do not meet this one's readers
-    if ((t & 63) == 0) rd[0][t >> 6] = mk, rd[1][t >> 6] = mv;
-    __syncthreads();
+    for (int i = 0; i < 16; ++i) mv = fmaxf(mv, fabsf(z[i / 4][i % 4]));
+    // the workgroup's maxima; two sets, so that the next head's do not meet
+    // this one's readers
+    auto meet = [&](int set) {
+      float(&rd)[2][NW] = red[set];
+      mk = wave_max(mk), mv = wave_max(mv);
+      if ((t & 63) == 0) rd[0][t >> 6] = mk, rd[1][t >> 6] = mv;
+      __syncthreads();
 #pragma unroll
-    for (int i = 0; i < NW; ++i) mk = fmaxf(mk, rd[0][i]), mv = fmaxf(mv, rd[1][i]);
+      for (int i = 0; i < NW; ++i) mk = fmaxf(mk, rd[0][i]), mv = fmaxf(mv, rd[1][i]);
+    };
+    meet(h & 1);
+    const bool inf = mk == INFINITY || mv == INFINITY;  // uniform; rare
+    if (inf) {
+      mk = mv = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) mk = fmaxf(mk, fmaxf(finite_abs(x[i]), finite_abs(y[i])));
+#pragma unroll
+      for (int i = 0; i < 16; ++i) mv = fmaxf(mv, finite_abs(z[i / 4][i % 4]));
+      __syncthreads();
+      meet(h & 1);
+      __syncthreads();
+    }
     const int ken = max(ke, exponent_for(mk)), ven = max(ve, exponent_for(mv));
     uint8_t* kt = a.pool.k + ti * 32 * DH;
     uint8_t* vt = a.pool.v + ti * 32 * DH;
-    // keys: [DH / 16][32][16]
-    const int c = j / 2, o = 8 * (j % 2);
-    uint2* k0 = reinterpret_cast<uint2*>(kt + (c * 32 + t % 32) * 16 + o);
-    uint2* k1 = reinterpret_cast<uint2*>(kt + ((c + DH / 32) * 32 + t % 32) * 16 + o);
-    if (krow >= 0) {
-      const float f = pow2i(-ken);
-      *k0 = make_uint2(pack_e4m3(x[0] * f, x[1] * f, x[2] * f, x[3] * f), pack_e4m3(x[4] * f, x[5] * f, x[6] * f, x[7] * f));
-      *k1 = make_uint2(pack_e4m3(y[0] * f, y[1] * f, y[2] * f, y[3] * f), pack_e4m3(y[4] * f, y[5] * f, y[6] * f, y[7] * f));
-    } else if (slot < len && ken > ke) {
-      const float f = pow2i(ke - ken);
-      const uint2 p = *k0, q = *k1;
-      *k0 = make_uint2(rescale_e4m3(p.x, f), rescale_e4m3(p.y, f));
-      *k1 = make_uint2(rescale_e4m3(q.x, f), rescale_e4m3(q.y, f));
-    }
-    // values: [DH][32], a word of 4 slots for each of 4 dims
-    {
-      const float f = pow2i(-ven), g2 = pow2i(ve - ven);
-      uint32_t keep = 0;  // bytes that stay
-      bool any_new = false, any_old = false;
+    auto put = [&](auto infinities) {
+      constexpr bool INF = decltype(infinities)::value;
+      // keys: [DH / 16][32][16]
+      const int c = j / 2, o = 8 * (j % 2);
+      uint2* k0 = reinterpret_cast<uint2*>(kt + (c * 32 + t % 32) * 16 + o);
+      uint2* k1 = reinterpret_cast<uint2*>(kt + ((c + DH / 32) * 32 + t % 32) * 16 + o);
+      if (krow >= 0) {
+        const float f = pow2i(-ken);
+        auto four = [&](const float* d) { return pack_e4m3<INF>(d[0] * f, d[1] * f, d[2] * f, d[3] * f); };
+        *k0 = make_uint2(four(x), four(x + 4));
+        *k1 = make_uint2(four(y), four(y + 4));
+      } else if (slot < len && ken > ke) {
+        const float f = pow2i(ke - ken);
+        const uint2 u = *k0, w = *k1;
+        *k0 = make_uint2(rescale_e4m3(u.x, f), rescale_e4m3(u.y, f));
+        *k1 = make_uint2(rescale_e4m3(w.x, f), rescale_e4m3(w.y, f));
+      }
+      // values: [DH][32], a word of 4 slots for each of 4 dims
+      const float f = pow2i(-ven), f_old = pow2i(ve - ven);
+      uint32_t keep = 0, older = 0;  // bytes that stay, bytes of earlier slots
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         if (vrow[i] < 0) keep |= 0xffu << (8 * i);
-        any_new |= vrow[i] >= 0;
-        any_old |= s0 + 4 * vg + i < len;
+        if (s0 + 4 * vg + i < len) older |= 0xffu << (8 * i);
       }
-      if (any_new || (any_old && ven > ve)) {
-        uint32_t older = 0;  // bytes of earlier slots
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (s0 + 4 * vg + i < len) older |= 0xffu << (8 * i);
-        const float* zf = &z[0].x;
+      if (keep != 0xffffffffu || (older && ven > ve)) {
 #pragma unroll
         for (int d = 0; d < 4; ++d) {
           uint32_t* w = reinterpret_cast<uint32_t*>(vt + (4 * vd + d) * 32 + 4 * vg);
-          auto at = [&](int i) { return d == 0 ? z[i].x : d == 1 ? z[i].y : d == 2 ? z[i].z : z[i].w; };
-          uint32_t u = pack_e4m3(at(0) * f, at(1) * f, at(2) * f, at(3) * f);
+          uint32_t u = pack_e4m3<INF>(z[0][d] * f, z[1][d] * f, z[2][d] * f, z[3][d] * f);
           if (keep) {
             uint32_t was = *w;
-            if (older && ven > ve) was = (was & ~older) | (rescale_e4m3(was, g2) & older);
+            if (older && ven > ve) was = (was & ~older) | (rescale_e4m3(was, f_old) & older);
             u = (u & ~keep) | (was & keep);
           }
           *w = u;
         }
       }
-    }
+    };
+    if (inf) put(std::true_type{});
+    else put(std::false_type{});
     if (t == 0) a.pool.ke[ti] = (int8_t)ken, a.pool.ve[ti] = (int8_t)ven;
+    now = next;
   }
+}
+
+template <int DH>
+void launch_dh(const PagedAppend& a, unsigned grid, hipStream_t s) {
+  if (a.dtype == PT_F32) hipLaunchKernelGGL((paged_append_kernel<DH, PT_F32>), dim3(grid), dim3(DH * 2), 0, s, a);
+  else if (a.dtype == PT_F16) hipLaunchKernelGGL((paged_append_kernel<DH, PT_F16>), dim3(grid), dim3(DH * 2), 0, s, a);
+  else hipLaunchKernelGGL((paged_append_kernel<DH, PT_BF16>), dim3(grid), dim3(DH * 2), 0, s, a);
 }
 
 }  // namespace
 
 hipError_t launch_paged_append(PagedAppend a, hipStream_t s) {
   const long long tiles = (long long)a.layers * a.batch * ((a.max_new + 31) / 32 + 1);
-  // One head per workgroup until there are enough of them, then all heads of a
-  // tile, which share the tile's sines.
-  a.heads_per_wg = (int)std::min<long long>(a.pool.Hkv, std::max<long long>(1, tiles * a.pool.Hkv / 1024));
+  // One head per workgroup until there are enough of them, then two, four ..,
+  // which share the tile's sines.
+  a.heads_per_wg = 1;
+  while (a.heads_per_wg < a.pool.Hkv && tiles * a.pool.Hkv / (2 * a.heads_per_wg) >= 2048) a.heads_per_wg *= 2;
   const long long grid = tiles * ((a.pool.Hkv + a.heads_per_wg - 1) / a.heads_per_wg);
   if (grid > 0x7fffffffLL) return hipErrorInvalidValue;
-  if (a.pool.dh == 128) hipLaunchKernelGGL(paged_append_kernel<128>, dim3((unsigned)grid), dim3(256), 0, s, a);
-  else if (a.pool.dh == 64) hipLaunchKernelGGL(paged_append_kernel<64>, dim3((unsigned)grid), dim3(128), 0, s, a);
+  if (a.pool.dh == 128) launch_dh<128>(a, (unsigned)grid, s);
+  else if (a.pool.dh == 64) launch_dh<64>(a, (unsigned)grid, s);
   else return hipErrorInvalidValue;
   return hipGetLastError();
 }
