@@ -521,10 +521,30 @@ typedef struct griffin_attention {
 size_t griffin_paged_attention_workspace(const griffin_attention *args);
 int griffin_paged_attention(const griffin_attention *args, void *workspace, size_t workspace_bytes, void *hip_stream);
 
+/* A verify context over an 8-bit paged cache.  pool: as above with a leading
+ * dimension of n_layers in all four buffers; its n_kv_heads and head_dim are
+ * the model's, and kv_capacity (a multiple of page_slots) is what a sequence's
+ * table can hold.  window, sinks: as for griffin_paged_attention (0: none).
+ * The context works as one of griffin_verify_init (steps, both acceptances,
+ * features, graphs), with these differences: a step writes nothing to the
+ * cache (the nodes' K/V stay with the context in fp32), and griffin_commit
+ * appends the root and the accepted nodes, rounded once.  A draft context may
+ * not be built on it.  Errors: as griffin_verify_init. */
+int griffin_verify_init_paged(const griffin_model_desc *desc, const griffin_weights *weights, const griffin_pool *pool,
+                              int32_t window, int32_t sinks, void *hip_stream, griffin_ctx **out);
+
+/* Set pages [first, first + n) of sequence seq's table (host array; -1: no
+ * page), in stream order: later steps and commits use them.  A step needs the
+ * pages of every slot that its nodes see and of the slots prefix_len ..
+ * prefix_len + depth that its commit may write, else it returns ECAPACITY.
+ * Sequences may share pages that they only read.  Errors: EINVAL (not a paged
+ * context, a page out of range), ECAPACITY (beyond kv_capacity), EHIP. */
+int griffin_set_pages(griffin_ctx *ctx, int32_t seq, int32_t first, int32_t n, const int32_t *pages);
+
 /* Kernel classes of one verification pass, for griffin_profile_*. */
 #define GRIFFIN_KC_QKV 0     /* QKV projection GEMM */
 #define GRIFFIN_KC_ROPE 1    /* rotary embedding + tree K/V write */
-#define GRIFFIN_KC_ATTN 2    /* prefix attention: split-KV partials */
+#define GRIFFIN_KC_ATTN 2    /* prefix attention: split-KV partials (paged cache: with their merge) */
 #define GRIFFIN_KC_O 3       /* output projection GEMM */
 #define GRIFFIN_KC_NORM 4    /* residual update + RMSNorm (and embedding; MoE: routing and dispatch) */
 #define GRIFFIN_KC_GATE_UP 5 /* gate/up GEMM with SwiGLU (MoE: routed experts) */

@@ -67,17 +67,19 @@ def tree_attention(q: np.ndarray, k: np.ndarray, v: np.ndarray, Kp: np.ndarray, 
 
 
 def verify_tree(ow: OracleWeights, prefix_kv: Callable[[int], Tuple[np.ndarray, np.ndarray]],
-                tree, prefix_len: int) -> VerifyResult:
+                tree, prefix_len: int, visible: Optional[np.ndarray] = None) -> VerifyResult:
     """Logits of every tree node.
 
     prefix_kv(l) returns the cached prefix of layer l as fp64 (K [Hkv, P, dh]
-    post-rotary, V [Hkv, P, dh])."""
+    post-rotary, V [Hkv, P, dh]); visible [T, P + T]: which keys each node sees
+    (None: the whole prefix and its root path)."""
     m = ow.shape
     T, P = tree.n, prefix_len
     Hq, Hkv, dh = m.n_q_heads, m.n_kv_heads, m.head_dim
     pos = P + tree.depths()
     vis = ancestor_matrix(tree.parents)
-    visible = np.concatenate([np.ones((T, P), dtype=bool), vis], axis=1)   # [T, P + T]
+    if visible is None:
+        visible = np.concatenate([np.ones((T, P), dtype=bool), vis], axis=1)   # [T, P + T]
 
     x = ow.embed(tree.tokens)
     tree_k, tree_v, routers = [], [], []

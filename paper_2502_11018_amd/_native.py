@@ -39,6 +39,11 @@ class Weights(ctypes.Structure):
     ]
 
 
+class Pool(ctypes.Structure):
+    _fields_ = [("k", c_void_p), ("v", c_void_p), ("k_exp", c_void_p), ("v_exp", c_void_p), ("n_pages", c_int32),
+                ("page_slots", c_int32), ("n_kv_heads", c_int32), ("head_dim", c_int32)]
+
+
 class DraftWeights(ctypes.Structure):
     _fields_ = [(n, c_void_p) for n in (
         "w_m", "b_m", "ln_h_g", "ln_h_b", "ln_x_g", "ln_x_b", "w_u", "b_u", "w_d", "b_d", "w_p", "b_p", "w_r", "b_r",
@@ -96,6 +101,9 @@ def _load() -> ctypes.CDLL:
         "griffin_draft_extend": (c_int32, [c_void_p, c_int32, I32P, I32P, I32P, c_void_p]),
         "griffin_draft_tree": (c_int32, [c_void_p, c_int32, I32P, I32P, c_void_p, c_int32, c_int32, c_int32, I32P,
                                          I32P, I32P, F32P]),
+        "griffin_verify_init_paged": (c_int32, [POINTER(ModelDesc), POINTER(Weights), POINTER(Pool), c_int32, c_int32,
+                                                c_void_p, POINTER(c_void_p)]),
+        "griffin_set_pages": (c_int32, [c_void_p, c_int32, c_int32, c_int32, I32P]),
         "griffin_paged_append": (c_int32, [c_char_p, c_void_p]),
         "griffin_paged_attention_workspace": (c_size_t, [c_char_p]),
         "griffin_paged_attention": (c_int32, [c_char_p, c_void_p, c_size_t, c_void_p]),
@@ -116,6 +124,6 @@ EXPORTED = ("griffin_kv_cache_bytes", "griffin_verify_init", "griffin_verify_ste
             "griffin_draft_tree", "griffin_read_features", "griffin_draft_extend",
             "griffin_set_activation_precision", "griffin_read_router_logits", "griffin_read_margins",
             "griffin_accept_sampled_walk_noalloc", "griffin_paged_append", "griffin_paged_attention",
-            "griffin_paged_attention_workspace")
+            "griffin_paged_attention_workspace", "griffin_verify_init_paged", "griffin_set_pages")
 KERNEL_CLASSES = ("qkv_gemm", "rope_kv_write", "tree_attention", "o_gemm", "residual_rmsnorm", "gate_up_gemm",
                   "down_gemm", "lm_head_gemm", "argmax_accept_route", "attn_merge")

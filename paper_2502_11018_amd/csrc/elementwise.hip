@@ -384,19 +384,23 @@ __global__ __launch_bounds__(256) void qkv_rope_kernel(const float* __restrict__
       q_lo[o + j] = f32_to_bf16(y1 - bf16_to_f32(h1));
       q_lo[o + j + half] = f32_to_bf16(y2 - bf16_to_f32(h2));
     } else {
-      uint16_t* k = kc + (((long long)b * Hkv + (h - Hq)) * kv_cap + slot) * dh;
-      k[j] = f32_to_bf16(y1);
-      k[j + half] = f32_to_bf16(y2);
+      if (kc) {  // a paged cache takes the accepted nodes at the commit
+        uint16_t* k = kc + (((long long)b * Hkv + (h - Hq)) * kv_cap + slot) * dh;
+        k[j] = f32_to_bf16(y1);
+        k[j + half] = f32_to_bf16(y2);
+      }
       float* k32 = tree.k + (((long long)b * Hkv + (h - Hq)) * max_tree + i) * dh;
       k32[j] = y1;
       k32[j + half] = y2;
     }
   } else {
     // 32-slot tiles, transposed within the tile: [tile][dim][32]
-    uint16_t* v = vc + ((long long)b * Hkv + (h - Hq - Hkv)) * dh * kv_cap + (long long)(slot >> 5) * dh * 32 +
-                  (slot & 31);
-    v[j * 32] = f32_to_bf16(x1);
-    v[(j + half) * 32] = f32_to_bf16(x2);
+    if (vc) {
+      uint16_t* v = vc + ((long long)b * Hkv + (h - Hq - Hkv)) * dh * kv_cap + (long long)(slot >> 5) * dh * 32 +
+                    (slot & 31);
+      v[j * 32] = f32_to_bf16(x1);
+      v[(j + half) * 32] = f32_to_bf16(x2);
+    }
     float* v32 = tree.v + (((long long)b * Hkv + (h - Hq - Hkv)) * max_tree + i) * dh;
     v32[j] = x1;
     v32[j + half] = x2;

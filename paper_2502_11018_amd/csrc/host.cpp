@@ -15,6 +15,8 @@
 
 #include "draft.h"
 #include "griffin_internal.h"
+#include "paged.h"
+#include "paged_host.h"
 #include "plan.h"
 #include "sampling.h"
 #include "griffin_verify.h"
@@ -155,7 +157,18 @@ struct griffin_ctx {
   float* margin_host = nullptr;    // pinned copy for griffin_read_margins
   float* router_logits = nullptr;  // MoE: [n_layers][max_batch * max_tree][E] fp32, the last pass's
   uint16_t *xn = nullptr, *q = nullptr, *q_lo = nullptr, *o = nullptr, *act = nullptr, *xe = nullptr;
-  TreeKV32 tree{};  // fp32 tree K/V of the layer being computed (reused by every layer)
+  TreeKV32 tree{};  // fp32 tree K/V of the layer being computed (reused by every layer; paged: of all layers)
+  // an 8-bit paged cache (griffin_verify_init_paged) instead of k_cache, v_cache
+  bool paged = false;
+  PagedPool pool{};             // layer 0
+  long long pool_layer = 0;     // tiles of one layer
+  int window = 0, sinks = 0, cols = 0;
+  int length_bound = 0;         // of this step's prefix lengths, a power of two or the capacity
+  std::vector<int32_t> table;   // [max_batch][cols] pages, -1: none
+  int32_t* table_dev = nullptr;
+  int32_t* table_host = nullptr;  // pinned staging
+  hipEvent_t table_ev = nullptr;
+  char* paged_ws = nullptr;
   int32_t *pidx = nullptr, *pnan = nullptr, *pred = nullptr, *nan_row = nullptr, *result = nullptr;
   int32_t *route_ids = nullptr, *count = nullptr, *slot = nullptr;
   // stochastic acceptance: residual rows [max_batch][2][vocab], uniforms
@@ -187,7 +200,7 @@ struct griffin_ctx {
     float* logits;
     bool kv_only;
     int tree_k, tree_depth, tree_n;  // 0: one pass
-    int slots;                       // partial slots the merge reads
+    int slots;                       // partial slots the merge reads (paged: the bound of the prefix lengths)
     int half;                        // griffin_ctx::half (a draft tree's passes set their own)
     hipGraphExec_t exec;
   };
@@ -340,6 +353,78 @@ int row_half(const griffin_ctx* c, int lo, int hi) {
   return hi <= 32 ? 1 : lo >= 32 ? 2 : 0;
 }
 
+// The bound of a step's prefix lengths that its launches are planned by: few
+// values, so few captured steps.
+int length_bound(int longest, int capacity) {
+  long long b = 256;
+  while (b < longest) b *= 2;
+  return (int)std::min<long long>(b, capacity);
+}
+
+// Whether every page that a step of sequence b reads, or that committing up to
+// `more` tokens behind its prefix writes, is set.
+bool has_pages(const griffin_ctx* c, int b, int prefix, int more) {
+  const int slots = c->pool.tpp * 32;
+  const int32_t* row = c->table.data() + (size_t)b * c->cols;
+  auto set = [&](long long lo, long long hi) {  // slots [lo, hi)
+    for (long long p = lo / slots; p * slots < hi; ++p)
+      if (row[p] < 0) return false;
+    return true;
+  };
+  const long long lo = c->window ? std::max(0, prefix - c->window + 1) : 0;
+  return set(lo, (long long)prefix + more) && set(0, std::min<long long>(c->window ? c->sinks : 0, prefix));
+}
+
+// A paged context's attention over `batch` sequences whose prefixes are at most
+// `bound` slots, without its buffers.
+int paged_shape(const griffin_ctx* c, int batch, int bound, PagedAttn* a) {
+  const griffin_model_desc& d = c->d;
+  *a = PagedAttn{};
+  a->pool = c->pool;
+  a->tab = PagedTable{c->table_dev, c->cols, c->cols, c->meta.prefix_len, bound};
+  a->dtype = PT_F32;
+  a->batch = batch;
+  a->nodes = d.max_tree;
+  a->Hq = d.n_q_heads;
+  a->cut.window = c->window;
+  a->cut.sinks = c->window ? c->sinks : 0;
+  return paged_plan(*a, bound);
+}
+
+// fp32 tree K/V elements of one layer
+size_t tree_layer(const griffin_model_desc& d) {
+  return (size_t)d.max_batch * d.n_kv_heads * d.max_tree * d.head_dim;
+}
+
+// [sequence][row][head] rows of a layer's tree K/V ([B][Hkv][max_tree][dh])
+PagedRows tree_rows(const griffin_model_desc& d, const float* p) {
+  const long long row = d.head_dim, head = (long long)d.max_tree * row;
+  return PagedRows{p, d.n_kv_heads * head, row, head, 1};
+}
+
+hipError_t paged_attention_of(griffin_ctx* c, int layer, float scale_log2, hipStream_t s) {
+  const griffin_model_desc& d = c->d;
+  PagedAttn a;
+  if (paged_shape(c, c->batch, c->length_bound, &a) != 0) return hipErrorInvalidValue;
+  const long long tiles = layer * c->pool_layer, bytes = tiles * 32 * d.head_dim;
+  a.pool.k += bytes;
+  a.pool.v += bytes;
+  a.pool.ke += tiles;
+  a.pool.ve += tiles;
+  a.counts = c->meta.n_nodes;
+  a.anc = c->meta.anc;
+  const long long head = d.head_dim, row = d.n_q_heads * head, seq = d.max_tree * row;
+  a.q = PagedRows{c->q, seq, row, head, 1};
+  a.q_lo = PagedRows{c->q_lo, seq, row, head, 1};
+  a.k = tree_rows(d, c->tree.k + layer * tree_layer(d));
+  a.v = tree_rows(d, c->tree.v + layer * tree_layer(d));
+  a.out = c->o;
+  a.out_ks = c->p_o.ks_pad;
+  a.scale_log2 = scale_log2;
+  paged_workspace(a, c->paged_ws);
+  return launch_paged_attention(a, s);
+}
+
 int enqueue_pass(griffin_ctx* c, float* logits_out) {
   const griffin_model_desc& d = c->d;
   const int B = c->batch;
@@ -378,13 +463,17 @@ int enqueue_pass(griffin_ctx* c, float* logits_out) {
       a.stamp = stamp_slot(c, GRIFFIN_KC_QKV);
       LAUNCH(GRIFFIN_KC_QKV, launch_plan(c->p_qkv, a, 1, s));
     }
-    uint16_t* kc = c->k_cache + (size_t)l * layer_kv;
-    uint16_t* vc = c->v_cache + (size_t)l * layer_kv;
+    uint16_t* kc = c->paged ? nullptr : c->k_cache + (size_t)l * layer_kv;
+    uint16_t* vc = c->paged ? nullptr : c->v_cache + (size_t)l * layer_kv;
+    const size_t tree_at = c->paged ? l * tree_layer(d) : 0;
+    const TreeKV32 tree{c->tree.k + tree_at, c->tree.v + tree_at};
     LAUNCH(GRIFFIN_KC_ROPE, launch_qkv_rope(c->parts, c->p_qkv.out_splits(m_tiles), ps * c->qkv_n, c->meta, c->rope_inv,
                                             d.n_q_heads, d.n_kv_heads, d.head_dim, d.max_tree, row0, nlive,
-                                            d.kv_capacity, c->q, c->q_lo, kc, vc, c->tree, s));
+                                            d.kv_capacity, c->q, c->q_lo, kc, vc, tree, s));
     if (c->kv_only && l == d.n_layers - 1) return GRIFFIN_OK;
-    {
+    if (c->paged) {
+      LAUNCH(GRIFFIN_KC_ATTN, paged_attention_of(c, l, scale_log2, s));
+    } else {
       AttnArgs a{};
       a.q = c->q;
       a.q_lo = c->q_lo;
@@ -404,11 +493,11 @@ int enqueue_pass(griffin_ctx* c, float* logits_out) {
       a.batch = B;
       a.scale_log2 = scale_log2;
       LAUNCH(GRIFFIN_KC_ATTN, launch_attention(a, B, s));
+      LAUNCH(GRIFFIN_KC_MERGE, launch_attn_combine(c->attn_po, c->attn_pml, c->meta, d.n_q_heads, d.n_kv_heads,
+                                                  d.head_dim, c->comb_slots, c->attn_sp, c->qblocks * 32, d.max_tree,
+                                                  row0, nlive, c->q, c->q_lo, tree, PrefixKV{kc, vc, d.kv_capacity},
+                                                  scale_log2, c->o, c->p_o.ks_pad, s));
     }
-    LAUNCH(GRIFFIN_KC_MERGE, launch_attn_combine(c->attn_po, c->attn_pml, c->meta, d.n_q_heads, d.n_kv_heads,
-                                                d.head_dim, c->comb_slots, c->attn_sp, c->qblocks * 32, d.max_tree,
-                                                row0, nlive, c->q, c->q_lo, c->tree, PrefixKV{kc, vc, d.kv_capacity},
-                                                scale_log2, c->o, c->p_o.ks_pad, s));
     {
       GemmArgs a = gemm_args(c->p_o, c->o, c->p_o.ks_pad, c->pk_o[l], m_tiles, !c->act_bf16);
       a.half = c->half;
@@ -566,7 +655,7 @@ int run_graph(griffin_ctx* c, const griffin_ctx::GraphEntry& key, Body body) {
 
 // One pass (batch, logits_out, kv_only from the context).
 int run_pass(griffin_ctx* c, float* logits_out) {
-  return run_graph(c, {c->batch, logits_out, c->kv_only, 0, 0, 0, c->comb_slots, c->half, nullptr},
+  return run_graph(c, {c->batch, logits_out, c->kv_only, 0, 0, 0, c->paged ? c->length_bound : c->comb_slots, c->half, nullptr},
                    [&]() { return enqueue_pass(c, logits_out); });
 }
 
@@ -719,15 +808,18 @@ void griffin_verify_free(griffin_ctx* c) {
   if (c->margin_host) hipHostFree(c->margin_host);
   if (c->samp_host) hipHostFree(c->samp_host);
   if (c->feat_rows_host) hipHostFree(c->feat_rows_host);
+  if (c->table_host) hipHostFree(c->table_host);
+  if (c->table_ev) hipEventDestroy(c->table_ev);
   if (c->feat_ev) hipEventDestroy(c->feat_ev);
   delete c;
 }
 
-int griffin_verify_init(const griffin_model_desc* desc, const griffin_weights* w, void* k_cache, void* v_cache,
-                        void* hip_stream, griffin_ctx** out) {
+// With a pool (k_cache, v_cache null) or with the two cache buffers.
+static int verify_init(const griffin_model_desc* desc, const griffin_weights* w, void* k_cache, void* v_cache,
+                       const griffin_pool* pages, int32_t window, int32_t sinks, void* hip_stream, griffin_ctx** out) {
   if (!out) return GRIFFIN_EINVAL;
   *out = nullptr;
-  if (!desc || !w || !k_cache || !v_cache) return GRIFFIN_EINVAL;
+  if (!desc || !w || (!pages && (!k_cache || !v_cache))) return GRIFFIN_EINVAL;
   std::string why;
   int rc = validate_desc(desc, &why);
   if (rc != GRIFFIN_OK) return rc;
@@ -746,9 +838,22 @@ int griffin_verify_init(const griffin_model_desc* desc, const griffin_weights* w
       if (!p || !aligned16(p)) return GRIFFIN_EINVAL;
   }
 
+  PagedPool pool{};
+  if (pages) {
+    rc = paged_pool_of(*pages, &pool);
+    if (rc != GRIFFIN_OK) return rc;
+    if (window < 0 || sinks < 0) return GRIFFIN_EINVAL;
+    if (pool.Hkv != d.n_kv_heads || pool.dh != d.head_dim || d.kv_capacity % pages->page_slots != 0) return GRIFFIN_ESHAPE;
+    if ((long long)d.max_batch * d.max_tree > (1 << 24) || (long long)d.n_q_heads * d.max_tree > (1 << 20)) return GRIFFIN_ESHAPE;
+  }
+
   griffin_ctx* c = new (std::nothrow) griffin_ctx();
   if (!c) return GRIFFIN_ENOMEM;
   c->d = d;
+  c->paged = pages != nullptr;
+  c->pool = pool;
+  c->window = window;
+  c->sinks = sinks;
   c->embed = static_cast<const uint16_t*>(w->embed);
   c->final_norm = static_cast<const uint16_t*>(w->final_norm);
   for (int l = 0; l < d.n_layers; ++l) {
@@ -819,11 +924,30 @@ int griffin_verify_init(const griffin_model_desc* desc, const griffin_weights* w
   ALLOC(c->parts, c->parts_elems);
   ALLOC(c->q, Mp * c->attn_w);
   ALLOC(c->q_lo, Mp * c->attn_w);
-  ALLOC(c->tree.k, (long long)d.max_batch * d.n_kv_heads * d.max_tree * d.head_dim);
-  ALLOC(c->tree.v, (long long)d.max_batch * d.n_kv_heads * d.max_tree * d.head_dim);
+  ALLOC(c->tree.k, tree_layer(d) * (c->paged ? d.n_layers : 1));
+  ALLOC(c->tree.v, tree_layer(d) * (c->paged ? d.n_layers : 1));
   ALLOC(c->o, tiles * c->p_o.ks_pad * XPACK_STEP);
-  ALLOC(c->attn_po, (long long)d.max_batch * d.n_q_heads * c->attn_sp * qrows * d.head_dim);
-  ALLOC(c->attn_pml, (long long)d.max_batch * d.n_q_heads * c->attn_sp * qrows * 2);
+  if (c->paged) {
+    c->pool_layer = (long long)pool.n_pages * pool.Hkv * pool.tpp;
+    c->cols = d.kv_capacity / pages->page_slots;
+    c->table.assign((size_t)d.max_batch * c->cols, -1);
+    size_t most = 0;  // of every batch and bound that a step can have
+    for (int b = 1; b <= d.max_batch; ++b)
+      for (int bound = length_bound(0, d.kv_capacity);; bound = length_bound(bound + 1, d.kv_capacity)) {
+        PagedAttn a;
+        if (paged_shape(c, b, bound, &a) != 0) {
+          griffin_verify_free(c);
+          return GRIFFIN_ESHAPE;
+        }
+        most = std::max(most, paged_workspace(a, nullptr));
+        if (bound == d.kv_capacity) break;
+      }
+    ALLOC(c->paged_ws, most);
+    ALLOC(c->table_dev, c->table.size());
+  } else {
+    ALLOC(c->attn_po, (long long)d.max_batch * d.n_q_heads * c->attn_sp * qrows * d.head_dim);
+    ALLOC(c->attn_pml, (long long)d.max_batch * d.n_q_heads * c->attn_sp * qrows * 2);
+  }
   ALLOC(c->act, (long long)c->E * tiles * c->p_down.ks_pad * XPACK_STEP);
   const long long lm_parts = (long long)c->p_lm.shape.n_wgs * c->p_lm.wn;
   ALLOC(c->pmax, Mp * lm_parts);
@@ -958,12 +1082,48 @@ int griffin_verify_init(const griffin_model_desc* desc, const griffin_weights* w
     griffin_verify_free(c);
     return GRIFFIN_ENOMEM;
   }
+  if (c->paged && (hipHostMalloc((void**)&c->table_host, sizeof(int32_t) * c->table.size(), hipHostMallocDefault) != hipSuccess ||
+                   hipEventCreateWithFlags(&c->table_ev, hipEventDisableTiming) != hipSuccess ||
+                   hipMemset(c->table_dev, 0xff, sizeof(int32_t) * c->table.size()) != hipSuccess)) {
+    griffin_verify_free(c);
+    return GRIFFIN_ENOMEM;
+  }
   hipError_t e = hipDeviceSynchronize();
   if (e != hipSuccess) {
     griffin_verify_free(c);
     return GRIFFIN_EHIP;
   }
   *out = c;
+  return GRIFFIN_OK;
+}
+
+int griffin_verify_init(const griffin_model_desc* desc, const griffin_weights* w, void* k_cache, void* v_cache,
+                        void* hip_stream, griffin_ctx** out) {
+  return verify_init(desc, w, k_cache, v_cache, nullptr, 0, 0, hip_stream, out);
+}
+
+int griffin_verify_init_paged(const griffin_model_desc* desc, const griffin_weights* w, const griffin_pool* pool,
+                              int32_t window, int32_t sinks, void* hip_stream, griffin_ctx** out) {
+  if (out) *out = nullptr;
+  if (!pool) return GRIFFIN_EINVAL;
+  return verify_init(desc, w, nullptr, nullptr, pool, window, sinks, hip_stream, out);
+}
+
+int griffin_set_pages(griffin_ctx* c, int32_t seq, int32_t first, int32_t n, const int32_t* pages) {
+  if (!c) return GRIFFIN_EINVAL;
+  if (!c->paged) return set_err(c, GRIFFIN_EINVAL, "the context has no paged cache");
+  if (seq < 0 || seq >= c->d.max_batch || first < 0 || n < 0 || (n > 0 && !pages))
+    return set_err(c, GRIFFIN_EINVAL, "bad sequence, range or null pages");
+  if ((long long)first + n > c->cols) return set_err(c, GRIFFIN_ECAPACITY, "pages beyond kv_capacity");
+  for (int i = 0; i < n; ++i)
+    if (pages[i] < -1 || pages[i] >= c->pool.n_pages) return set_err(c, GRIFFIN_EINVAL, "page out of range");
+  if (n == 0) return GRIFFIN_OK;
+  const size_t at = (size_t)seq * c->cols + first;
+  HIP_TRY(c, hipEventSynchronize(c->table_ev));  // the staging's last copy
+  std::copy(pages, pages + n, c->table.begin() + at);
+  std::copy(pages, pages + n, c->table_host + at);
+  HIP_TRY(c, hipMemcpyAsync(c->table_dev + at, c->table_host + at, sizeof(int32_t) * n, hipMemcpyHostToDevice, c->stream));
+  HIP_TRY(c, hipEventRecord(c->table_ev, c->stream));
   return GRIFFIN_OK;
 }
 
@@ -975,13 +1135,17 @@ int griffin_verify_step(griffin_ctx* c, int32_t batch, const int32_t* prefix_len
     return set_err(c, GRIFFIN_EINVAL, "bad batch or null host array");
   if (logits_out && !aligned16(logits_out)) return set_err(c, GRIFFIN_EINVAL, "logits_out not 16-byte aligned");
   // validate everything before touching any buffer
+  int32_t depth[kMaxTree];
   for (int b = 0; b < batch; ++b) {
     std::string why;
     const int rc = prepare_tree(n_nodes[b], tokens + (size_t)b * d.max_tree, parents + (size_t)b * d.max_tree,
-                                prefix_len[b], d.max_tree, d.max_depth, d.vocab, d.kv_capacity, nullptr, nullptr,
+                                prefix_len[b], d.max_tree, d.max_depth, d.vocab, d.kv_capacity, depth, nullptr,
                                 nullptr, &why);
     if (rc != GRIFFIN_OK) return set_err(c, rc, "sequence " + std::to_string(b) + ": " + why);
+    if (c->paged && !has_pages(c, b, prefix_len[b], *std::max_element(depth, depth + n_nodes[b]) + 1))
+      return set_err(c, GRIFFIN_ECAPACITY, "sequence " + std::to_string(b) + ": a page of the step is not set");
   }
+  if (c->paged) c->length_bound = length_bound(*std::max_element(prefix_len, prefix_len + batch), d.kv_capacity);
   // fill the staging buffer not used by the previous step's copy
   const int k = c->meta_cur ^ 1;
   HIP_TRY(c, hipEventSynchronize(c->meta_ev[k]));
@@ -1031,6 +1195,29 @@ int griffin_commit(griffin_ctx* c) {
   if (!c->accepted)
     return set_err(c, GRIFFIN_EORDER, "no griffin_accept or griffin_accept_sampled since the last step");
   const griffin_model_desc& d = c->d;
+  if (c->paged) {
+    // the root and the accepted nodes, of every layer, from the fp32 tree K/V
+    PagedAppend a{};
+    a.pool = c->pool;
+    a.tab = PagedTable{c->table_dev, c->cols, c->cols, c->meta.prefix_len, d.kv_capacity};
+    a.counts = c->accepted;
+    a.counts_stride = result_stride(d.max_depth);
+    a.counts_add = 1;
+    a.path = c->accepted + 3 + d.max_depth;
+    a.path_stride = a.counts_stride;
+    a.path_first = 1;
+    a.k = tree_rows(d, c->tree.k);
+    a.v = tree_rows(d, c->tree.v);
+    a.dtype = PT_F32;
+    a.batch = c->batch;
+    a.rows = d.max_tree;
+    a.max_new = d.max_depth + 1;
+    a.layers = d.n_layers;
+    a.pool_layer = c->pool_layer;
+    a.rows_layer = (long long)tree_layer(d);
+    HIP_TRY(c, launch_paged_append(a, c->stream));
+    return GRIFFIN_OK;
+  }
   const long long layer_kv = (long long)d.max_batch * d.n_kv_heads * d.kv_capacity * d.head_dim;
   HIP_TRY(c, launch_commit(c->accepted, d.max_depth, c->meta, c->batch, d.n_layers, d.n_kv_heads, d.head_dim,
                            d.kv_capacity, layer_kv, c->k_cache, c->v_cache, c->stream));

@@ -66,7 +66,7 @@ class SpeculativeCycle:
         self.logits = None
         if self.temperature > 0:
             self.logits = torch.empty((verifier.max_batch * verifier.max_tree, verifier.shape.vocab),
-                                      dtype=torch.float32, device=verifier.k_cache.device)
+                                      dtype=torch.float32, device=verifier.device)
         self.prefix: List[int] = []
         self.roots: List[int] = []
         self.root_features = None

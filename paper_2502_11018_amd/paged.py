@@ -32,14 +32,21 @@ class PagedPool(NamedTuple):
     v_exp: torch.Tensor
 
 
-def paged_pool(n_pages: int, n_kv_heads: int, head_dim: int, page: int = 64, device="cuda") -> PagedPool:
-    """An empty pool of one layer."""
+def paged_pool(n_pages: int, n_kv_heads: int, head_dim: int, page: int = 64, device="cuda",
+               layers: Optional[int] = None) -> PagedPool:
+    """An empty pool of one layer; layers: of that many, as a leading dimension
+    of its tensors (what a paged TreeVerifier takes; layer_pool gives one)."""
     if n_pages < 1 or n_kv_heads < 1 or head_dim not in (64, 128) or page < 32 or page % 32:
         raise ValueError("a pool needs pages and heads, head_dim 64 or 128 and pages of a multiple of 32 slots")
-    tiles = (n_pages, n_kv_heads, page // 32)
+    tiles = (() if layers is None else (layers,)) + (n_pages, n_kv_heads, page // 32)
     byte = lambda *s: torch.zeros(tiles + s, dtype=torch.uint8, device=device).view(_E4M3)  # noqa: E731
     exps = lambda: torch.full(tiles, -110, dtype=torch.int8, device=device)  # noqa: E731
     return PagedPool(byte(head_dim // 16, 32, 16), byte(head_dim, 32), exps(), exps())
+
+
+def layer_pool(pool: Sequence[torch.Tensor], layer: int) -> PagedPool:
+    """One layer of a pool of several."""
+    return PagedPool(*(t[layer] for t in pool))
 
 
 def paged_read(pool: Sequence[torch.Tensor], table: torch.Tensor, n: int):

@@ -15,6 +15,7 @@ import numpy as np
 import torch
 
 from . import _native as N
+from .paged import _pool_fields, layer_pool, paged_append
 
 
 def _i32(a) -> np.ndarray:
@@ -153,11 +154,15 @@ class TreeVerifier:
            vocab, n_experts, top_k, rms_eps, rope_base.
     weights: object with embed, lm_head, final_norm (bf16 CUDA tensors) and
            layers[l] = dict(attn_norm, w_qkv, w_o, mlp_norm, w_gate_up, w_down, w_router).
+    pool: an 8-bit paged cache of n_layers layers (paged_pool(..., layers=))
+           instead of k_cache and v_cache; kv_capacity is then what a
+           sequence's page table holds, set_pages says which pages those are,
+           and window / sinks bound what the nodes see.
     """
 
     def __init__(self, shape, weights, *, max_batch: int, max_tree: int, max_depth: int, kv_capacity: int,
                  k_cache: Optional[torch.Tensor] = None, v_cache: Optional[torch.Tensor] = None,
-                 stream: Optional[torch.cuda.Stream] = None):
+                 stream: Optional[torch.cuda.Stream] = None, pool=None, window: int = 0, sinks: int = 0):
         self.shape = shape
         self.max_batch, self.max_tree, self.max_depth, self.kv_capacity = max_batch, max_tree, max_depth, kv_capacity
         self.desc = N.ModelDesc(shape.n_layers, shape.d_model, shape.n_q_heads, shape.n_kv_heads, shape.head_dim,
@@ -167,12 +172,26 @@ class TreeVerifier:
         if dev.type != "cuda":
             raise ValueError("weights must be device tensors")
         L, Hkv, dh = shape.n_layers, shape.n_kv_heads, shape.head_dim
-        if k_cache is None:
+        self.device, self.pool = dev, pool
+        if pool is not None:
+            if k_cache is not None or v_cache is not None:
+                raise ValueError("a cache is k_cache and v_cache, or a pool")
+            fields, heads, pool_dh, pool_dev = _pool_fields(layer_pool(pool, 0))
+            if any(t.dim() < 4 or t.shape[0] != L or not t.is_contiguous() for t in pool) or pool_dev != dev:
+                raise ValueError(f"the pool's tensors must be contiguous with {L} layers on {dev}")
+            page = fields[5]
+            if kv_capacity % page:
+                raise ValueError("kv_capacity must be a multiple of the pool's page")
+            self._pool_desc = N.Pool(*(t.data_ptr() for t in pool), fields[4], page, heads, pool_dh)
+            self.pages = np.full((max_batch, kv_capacity // page), -1, dtype=np.int32)
+        elif window or sinks:
+            raise ValueError("a window needs a paged cache (pool)")
+        elif k_cache is None:
             k_cache = torch.zeros((L, max_batch, Hkv, kv_capacity, dh), dtype=torch.bfloat16, device=dev)
-        if v_cache is None:
+        if v_cache is None and pool is None:
             v_cache = torch.zeros((L, max_batch, Hkv, kv_capacity // 32, dh, 32), dtype=torch.bfloat16, device=dev)
         need = N.lib.griffin_kv_cache_bytes(byref(self.desc))
-        for t in (k_cache, v_cache):
+        for t in (k_cache, v_cache) if pool is None else ():
             if t.dtype != torch.bfloat16 or not t.is_contiguous() or t.numel() * 2 != need:
                 raise ValueError("KV cache tensors must be contiguous bf16 of griffin_kv_cache_bytes bytes")
         self.k_cache, self.v_cache = k_cache, v_cache
@@ -194,9 +213,13 @@ class TreeVerifier:
         # init repacks the weights on the library's stream: order it after the
         # caller's stream, where the weights and caches were produced
         self.stream.wait_stream(torch.cuda.current_stream(dev))
-        rc = N.lib.griffin_verify_init(byref(self.desc), byref(self.w), k_cache.data_ptr(), v_cache.data_ptr(),
-                                       c_void_p(self.stream.cuda_stream), byref(self.ctx))
-        _check(rc, "griffin_verify_init")
+        if pool is not None:
+            rc = N.lib.griffin_verify_init_paged(byref(self.desc), byref(self.w), byref(self._pool_desc), window, sinks,
+                                                 c_void_p(self.stream.cuda_stream), byref(self.ctx))
+        else:
+            rc = N.lib.griffin_verify_init(byref(self.desc), byref(self.w), k_cache.data_ptr(), v_cache.data_ptr(),
+                                           c_void_p(self.stream.cuda_stream), byref(self.ctx))
+        _check(rc, "griffin_verify_init" if pool is None else "griffin_verify_init_paged")
         self._batch = 0
 
     # ------------------------------------------------------------ KV cache ----
@@ -205,9 +228,27 @@ class TreeVerifier:
         return self.v_cache.view(self.shape.n_layers, self.max_batch, Hkv, self.kv_capacity // 32, dh, 32)[layer, seq]
 
     def write_prefix(self, layer: int, seq: int, k: torch.Tensor, v: torch.Tensor):
-        """Place a cached prefix: k, v bf16 [Hkv, P, dh] (k post-rotary)."""
+        """Place a cached prefix: k, v bf16 [Hkv, P, dh] (k post-rotary).  Paged:
+        in the sequence's pages, rounded to 8 bits (fp16 and fp32 too)."""
+        if self.pool is not None:
+            n = -(-k.shape[1] // self._pool_desc.page_slots)
+            if (self.pages[seq, :n] < 0).any():
+                raise ValueError("write_prefix: a page of the prefix is not set")
+            table = torch.from_numpy(self.pages[seq:seq + 1, :n].copy()).to(self.device)
+            paged_append(layer_pool(self.pool, layer), table, torch.zeros(1, dtype=torch.int32, device=self.device),
+                         k.transpose(0, 1)[None], v.transpose(0, 1)[None], stream=self.stream)
+            self.stream.synchronize()  # table, and the caller's tensors, end here
+            return
         write_prefix(self.k_cache, self.v_cache, self.shape, self.max_batch, self.kv_capacity, layer, seq, k, v,
                      self.stream)
+
+    def set_pages(self, seq: int, pages, first: int = 0):
+        """Paged cache: pages `first` .. of sequence seq's table (-1: none), for
+        what is enqueued from now on."""
+        pages = _i32(pages)
+        rc = N.lib.griffin_set_pages(self.ctx, seq, first, len(pages), _p32(pages))
+        _check(rc, "griffin_set_pages", self.ctx)
+        self.pages[seq, first:first + len(pages)] = pages
 
     def read_v(self, layer: int, seq: int, n: int) -> torch.Tensor:
         """Cached values of slots [0, n) as [Hkv, n, dh]."""
@@ -304,7 +345,7 @@ class TreeVerifier:
         if ids.ndim != 2:
             raise ValueError("nodes must be a [batch][n] array")
         B, n = ids.shape
-        out = torch.empty((B, n, self.shape.d_model), dtype=torch.float32, device=self.k_cache.device)
+        out = torch.empty((B, n, self.shape.d_model), dtype=torch.float32, device=self.device)
         ids = np.ascontiguousarray(ids)
         rc = N.lib.griffin_read_features(self.ctx, B, n, _p32(ids), c_void_p(out.data_ptr()))
         _check(rc, "griffin_read_features", self.ctx)

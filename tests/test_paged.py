@@ -139,6 +139,38 @@ def test_attention_wants_its_workspace():
     assert N.lib.griffin_paged_attention(None, 256, need, None) == N.CODES["GRIFFIN_EINVAL"]
 
 
+def test_paged_context_refuses():
+    """griffin_verify_init_paged and griffin_set_pages, before any device work."""
+    from ctypes import byref, c_void_p
+    N = _lib()
+    ctx, w = c_void_p(), N.Weights()
+    desc = N.ModelDesc(2, 256, 4, 4, 64, 688, 1024, 1, 1, 1e-6, 1e4, 1, 16, 4, 192)
+    init = lambda pool, window=0, sinks=0: N.lib.griffin_verify_init_paged(  # noqa: E731
+        byref(desc), byref(w), byref(pool) if pool else None, window, sinks, None, byref(ctx))
+    assert init(None) == N.CODES["GRIFFIN_EINVAL"]
+    assert init(N.Pool(16, 16, 16, 16, 4, 64, 4, 64)) == N.CODES["GRIFFIN_EINVAL"]      # null weights
+    assert N.lib.griffin_verify_init_paged(None, byref(w), byref(N.Pool(16, 16, 16, 16, 4, 64, 4, 64)), 0, 0, None,
+                                           byref(ctx)) == N.CODES["GRIFFIN_EINVAL"]
+    # every weight pointer set (never followed): the pool's own checks
+    ptrs = (c_void_p * 2)(16, 16)
+    import ctypes
+    cast = ctypes.cast(ptrs, ctypes.POINTER(c_void_p))
+    w = N.Weights(16, 16, 16, cast, cast, cast, cast, cast, cast, None)
+    for pool, window, sinks, code in [
+            (N.Pool(16, 16, 16, 16, 4, 64, 2, 64), 0, 0, "ESHAPE"),      # heads
+            (N.Pool(16, 16, 16, 16, 4, 64, 4, 128), 0, 0, "ESHAPE"),     # head_dim
+            (N.Pool(16, 16, 16, 16, 4, 128, 4, 64), 0, 0, "ESHAPE"),     # 192 slots are no whole pages
+            (N.Pool(16, 16, 16, 16, 4, 40, 4, 64), 0, 0, "ESHAPE"),
+            (N.Pool(16, 16, 16, 16, 0, 64, 4, 64), 0, 0, "ESHAPE"),
+            (N.Pool(16, 8, 16, 16, 4, 64, 4, 64), 0, 0, "EINVAL"),       # alignment
+            (N.Pool(16, 16, None, 16, 4, 64, 4, 64), 0, 0, "EINVAL"),
+            (N.Pool(16, 16, 16, 16, 4, 64, 4, 64), -1, 0, "EINVAL"),
+            (N.Pool(16, 16, 16, 16, 4, 64, 4, 64), 5, -1, "EINVAL")]:
+        assert init(pool, window, sinks) == N.CODES["GRIFFIN_" + code]
+        assert not ctx.value
+    assert N.lib.griffin_set_pages(None, 0, 0, 0, None) == N.CODES["GRIFFIN_EINVAL"]
+
+
 def test_binding_checks_tensors():
     """The Python calls refuse tensors before the library sees an address."""
     import paper_2502_11018_amd as G
