@@ -624,7 +624,9 @@ __global__ __launch_bounds__(256, 2) void paged_attention_kernel(PagedAttn a) {
 //   the scores of tile i + 1, between the softmax of tile i;
 //   O += V P of tile i, between the conversion of its values, the reads of tile
 //   i + 2's keys and the maximum of tile i + 1's scores, which decides whether
-//   a reference has to rise: no branch stands inside a step.
+//   a reference has to rise: no branch stands inside a step.  At a higher
+//   priority, so that one wave's matrix work goes before the other's softmax
+//   (148 -> 142 us for 8 x 61 nodes over 16384 slots).
 // The workgroup meets once in two tiles (2 p, 2 p + 1): then every wave has its
 // share of pair p + 2 and is done with pair p, whose slots pair p + D / 2 gets.
 // Tiles that not every row sees whole are computed one by one before.
@@ -791,6 +793,7 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_wide_kernel(PagedAttn a) {
         __builtin_amdgcn_sched_barrier(0);
       }
       if constexpr (QF == Q_SPLIT) sn += lo;
+      __builtin_amdgcn_s_setprio(1);
       constexpr int PL = probs_split(QF) ? 2 : 1, S2 = 2 * DB * PL;  // O += V P: half, dims, part
       constexpr int S3 = S2 - 2;                                     // the maximum is there two MFMAs before the end
       u32x4 v16 = zero_u4();
@@ -806,6 +809,7 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_wide_kernel(PagedAttn a) {
         }
         __builtin_amdgcn_sched_barrier(0);
       }
+      __builtin_amdgcn_s_setprio(0);
       far = beyond(mx, fn, exn);
       f = fn;
       ex = exn;
