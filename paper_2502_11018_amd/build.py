@@ -25,7 +25,7 @@ ARCH = "gfx950"
 # Accumulators in the vector registers although a wave holds more than 256 in
 # all: with them in the accumulation registers every score costs a move before
 # the softmax can read it.
-FILE_FLAGS = {name: ["-mllvm", "-amdgpu-mfma-vgpr-form"] for name in ("attention.hip", "paged_attention.hip")}
+FILE_FLAGS = {name: ["-mllvm", "-amdgpu-mfma-vgpr-form"] for name in ("attention.hip", "paged_attention.hip", "paged_thin.hip")}
 
 
 def hipcc() -> str:

@@ -95,10 +95,13 @@ struct PagedAttn {
   float* part_o;          // [units][Hkv][G * nodes][dh]
   float* part_ml;         // [units][Hkv][G * nodes][2]
   int2* first_unit;       // [batch] first unit and units of a sequence that has any
-  int wide;               // waves of a workgroup of the wide kernel, 0: the other one (paged_plan)
+  // the kernel (paged_plan): at most 16 rows a KV head: thin, fused where it needs no joining; else
+  // wide: waves of a workgroup of the wide kernel, or 0
+  int thin, fused, wide;
   int32_t* status;
 };
 hipError_t launch_paged_attention(const PagedAttn& a, hipStream_t s);
+hipError_t launch_paged_thin(const PagedAttn& a, hipStream_t s);
 
 // Shape of the call, from host values alone: fills a.cut, a.units and the
 // workgroup's shape.  Not 0: too many tiles.

@@ -32,123 +32,11 @@
 
 #include <algorithm>
 
-#include "griffin_internal.h"
-#include "paged.h"
+#include "paged_device.h"
 
 namespace griffin {
 
 namespace {
-
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
-typedef int i32x8 __attribute__((ext_vector_type(8)));
-struct KeyPair {
-  u32x4 a, b;
-};
-__device__ __forceinline__ f16x8 as_f16x8(const u32x4& v) { return __builtin_bit_cast(f16x8, v); }
-
-// The cached tiles that some node of a sequence of `len` slots sees: the first
-// `sink` ones, then those from `lo` on; n in all.
-struct SeqTiles {
-  int n, sink, lo;
-};
-__host__ __device__ inline SeqTiles seq_tiles(int len, const PagedCut& c) {
-  const int all = (int)(((long long)len + 31) >> 5);
-  if (c.window == 0) return {all, 0, 0};
-  const int lo = max(0, len - c.window + 1) >> 5;  // the root's window starts first
-  const int sink = min((int)(((long long)c.sinks + 31) >> 5), lo);
-  return {sink + all - lo, sink, lo};
-}
-
-// A sequence's length as the kernels use it: 0 where it is out of range.
-__device__ __forceinline__ int checked_len(const PagedTable& t, int b, bool* bad) {
-  const int len = t.lengths[b];
-  const bool ok = len >= 0 && len <= t.most;
-  if (!ok) *bad = true;
-  return ok ? len : 0;
-}
-
-// Sum over the lanes that hold sequences (uniform; whole waves call these).
-__device__ __forceinline__ int lanes_sum(int n, int batch) {
-  for (int o = 1; o < 64 && o < batch; o <<= 1) n += __shfl_xor(n, o, 64);
-  return __builtin_amdgcn_readfirstlane(n);
-}
-
-// The sequence of unit u: {sequence (-1: none), split, splits}.  A unit holds
-// at most `per` tiles, and a sequence's units the same number each to one;
-// per is at least ceil(all tiles / target), and rises for a few steps while
-// the sequences' last units bring their number above the target (workgroups
-// that do not fit the chip at once cost a second round: 18.5 -> 14.1 us for 16
-// sequences of up to 2048 slots).
-struct UnitAt {
-  int b, split, n;
-};
-__device__ UnitAt unit_at(const PagedAttn& a, int u) {
-  const int lane = threadIdx.x & 63;
-  bool bad = false;
-  auto tiles = [&](int b) { return b < a.batch ? seq_tiles(checked_len(a.tab, b, &bad), a.cut).n : 0; };
-  const int own = tiles(lane);
-  uint32_t total = lanes_sum(own, a.batch);
-  for (int b0 = 64; b0 < a.batch; b0 += 64) total += lanes_sum(tiles(b0 + lane), 64);
-  // half the target while units are short: a unit's start and join cost more
-  // than what the second workgroup of a CU hides
-  const uint32_t target = total >= (uint32_t)a.cut.target * a.cut.full ? a.cut.target : (a.cut.target + 1) / 2;
-  uint32_t per = max((uint32_t)a.cut.least, (total + target - 1) / target);
-  for (int i = 0; i < 4; ++i) {
-    uint32_t units = 0;
-    for (int b0 = 0; b0 < a.batch; b0 += 64)
-      units += lanes_sum(((b0 ? tiles(b0 + lane) : own) + per - 1) / per, b0 ? 64 : a.batch);
-    if (units <= target) break;
-    per += (per * (units - target) + target - 1) / target;
-  }
-  int first = 0;
-  for (int b0 = 0; b0 < a.batch; b0 += 64) {
-    const int n = ((b0 ? tiles(b0 + lane) : own) + per - 1) / per;
-    int end = n;  // inclusive sum over the lanes
-    for (int o = 1; o < 64 && o < a.batch; o <<= 1) {
-      const int y = __shfl_up(end, o, 64);
-      if (lane >= o) end += y;
-    }
-    const unsigned long long in = __ballot(u >= first + end - n && u < first + end);
-    if (in) {
-      const int l = __builtin_ctzll(in);
-      return {b0 + l, u - first - __builtin_amdgcn_readlane(end - n, l), __builtin_amdgcn_readlane(n, l)};
-    }
-    first += __builtin_amdgcn_readlane(end, 63);
-  }
-  return {-1, 0, 0};
-}
-
-// 8 e4m3 of two words as fp16 or bf16 (both exact), times 2^e of the factor `s`
-__device__ __forceinline__ f16x8 cvt8(uint32_t a, uint32_t b, float s) {
-  const f16x2 p = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, s, false), q = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, s, true);
-  const f16x2 r = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, s, false), t = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, s, true);
-  return f16x8{p.x, p.y, q.x, q.y, r.x, r.y, t.x, t.y};
-}
-__device__ __forceinline__ bf16x8 cvt8_bf16(uint32_t a, uint32_t b) {
-  const bf16x2 p = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.f, false), q = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.f, true);
-  const bf16x2 r = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.f, false), t = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.f, true);
-  return bf16x8{p.x, p.y, q.x, q.y, r.x, r.y, t.x, t.y};
-}
-
-// nodes that node i sees, and its position behind the cached slots
-__device__ __forceinline__ uint64_t anc_of(const PagedAttn& a, int b, int i) {
-  return a.anc ? a.anc[(long long)b * a.nodes + i] & (~0ull >> (64 - a.nodes)) : (2ull << i) - 1;
-}
-__device__ __forceinline__ int depth_of(uint64_t anc, int i) { return __builtin_popcountll(anc & ~(1ull << i)); }
-
-constexpr float NO_MAX = -3e38f;  // reference of a row that has seen no key
-
-// How q enters the matrix cores, by its type and the kernel:
-//   Q_BF16   bf16 as it is, keys converted to bf16
-//   Q_FP8    bf16 as two e4m3 parts (4 + 4 bits, exact down to 2^-21 of the row's largest value), keys
-//            not converted at all: for waves with many tiles, as splitting q costs what converting
-//            the keys of a dozen tiles does
-//   Q_F16    fp16 as it is
-//   Q_SPLIT  fp32 (or bf16 hi + lo) as two fp16 parts
-enum QueryForm : int { Q_BF16, Q_FP8, Q_F16, Q_SPLIT };
-
-constexpr bool probs_split(int qf) { return qf == Q_F16 || qf == Q_SPLIT; }  // probabilities as two fp16 parts
 
 // A tile in a wave's registers, as it is stored: 1 KB pieces, 16 bytes a lane.
 template <int DH>
@@ -194,10 +82,8 @@ struct Query {
           for (int i = 0; i < 8; ++i) mx = fmaxf(mx, fabsf(v[x][h][i]));
         }
       mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-      // the row's largest value to [2^TOP, 2^(TOP + 1)); subnormal rows stay
-      // near zero, infinite ones infinite
-      constexpr int TOP = QF == Q_FP8 ? 7 : 8;
-      const int ex = min(max((int)(__float_as_uint(mx) >> 23) - 127, -110), 118);
+      constexpr int TOP = QF == Q_FP8 ? 7 : 8;  // the row's largest value to [2^TOP, 2^(TOP + 1))
+      const int ex = scale_exponent(mx);
       const float f = pow2i(TOP - ex);
       fac *= pow2i(ex - TOP);
 #pragma unroll
@@ -208,10 +94,9 @@ struct Query {
           for (int i = 0; i < 8; i += 2) {
             const float v0 = v[x][h][i] * f, v1 = v[x][h][i + 1] * f;
             if constexpr (QF == Q_SPLIT) {
-              const f16x2 hi = __builtin_convertvector(f32x2{v0, v1}, f16x2);
-              const f16x2 lo = __builtin_convertvector(f32x2{v0 - (float)hi.x, v1 - (float)hi.y}, f16x2);
-              a[x][h][i / 2] = __builtin_bit_cast(uint32_t, hi);
-              b[x][h][i / 2] = __builtin_bit_cast(uint32_t, lo);
+              const Hilo2 parts = split_f16(v0, v1);
+              a[x][h][i / 2] = parts.hi;
+              b[x][h][i / 2] = parts.lo;
             } else {
               // word i / 4 of the half, its lower or upper pair; the low part
               // 2^4 up, which its product's scale takes back
@@ -308,24 +193,6 @@ struct State {
       E = ve;
     }
   }
-};
-
-// A score's factor on a tile: never 0, which times a masked -inf would be a NaN.
-__device__ __forceinline__ float score_factor(float fac, int ke) { return fmaxf(fac * pow2i(ke), 0x1p-126f); }
-
-// The places of a tile that a row does not see, for lane half hh.
-struct Sight {
-  int len, window, sinks;
-  __device__ __forceinline__ bool of(int slot, int pos) const {
-    return slot < len && (window == 0 || slot > pos - window || slot < sinks);
-  }
-};
-
-struct Edge {
-  static constexpr bool value = true;
-};
-struct Whole {
-  static constexpr bool value = false;
 };
 
 // Softmax of one tile's scores and O^T += V^T P^T.  EDGE: a tile (first slot
@@ -425,53 +292,6 @@ __device__ __forceinline__ void attend(State<DH>& st, f32x16 s, Vals<DH> v, floa
       if constexpr (probs_split(QF)) st.o[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v8, as_f16x8(pl), st.o[x], 0, 0, 0);
     }
   }
-}
-
-// Where a workgroup works: unit u (sequence b, the list's tiles [i0, i1)) of KV
-// head hk, row block rb.
-struct Place {
-  int u, b, hk, rb, i0, i1;
-  SeqTiles seq;
-  Sight sight;
-  bool bad;
-};
-__device__ __forceinline__ bool place_of(const PagedAttn& a, int blocks, Place& p) {
-  // XCD-aware decode: workgroups go round-robin over the 8 XCDs, so the row
-  // blocks of one (unit, KV head) get the same id % 8 and share its L2
-  const int id = blockIdx.x, rest = id >> 3;
-  p.rb = rest % blocks;
-  const int st = (rest / blocks) * 8 + (id & 7);
-  p.hk = st % a.pool.Hkv;
-  p.u = st / a.pool.Hkv;
-  const UnitAt at = unit_at(a, p.u);
-  if (at.b < 0) return false;  // uniform
-  p.b = at.b;
-  p.bad = false;
-  const int len = checked_len(a.tab, at.b, &p.bad);
-  p.seq = seq_tiles(len, a.cut);
-  p.i0 = (int)((long long)p.seq.n * at.split / at.n);
-  p.i1 = (int)((long long)p.seq.n * (at.split + 1) / at.n);
-  p.sight = Sight{len, a.cut.window, a.cut.sinks};
-  // the joining kernel finds a sequence's units here
-  if (at.split == 0 && p.hk == 0 && p.rb == 0 && threadIdx.x == 0) a.first_unit[at.b] = make_int2(p.u, at.n);
-  return true;
-}
-
-// The tile that entry i of a sequence's list is, and its number in the pool.
-struct TileAt {
-  int tile, at;
-};
-__device__ __forceinline__ TileAt look_up(const PagedAttn& a, Place& p, int i) {
-  TileAt t;
-  t.tile = i < p.seq.sink ? i : i - p.seq.sink + p.seq.lo;
-  int page = a.tab.pages[(long long)p.b * a.tab.stride + t.tile / a.pool.tpp];
-  if (page < 0 || page >= a.pool.n_pages) {
-    p.bad = true;
-    if (a.status) atomicOr(a.status, PAGED_BAD_PAGE);
-    page = 0;
-  }
-  t.at = (page * a.pool.Hkv + p.hk) * a.pool.tpp + t.tile % a.pool.tpp;
-  return t;
 }
 
 // MFMA row -> slot of the tile: row 8q + 4h + e holds slot 16h + 4q + e
@@ -855,9 +675,8 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_wide_kernel(PagedAttn a) {
 // they meet in LDS.  What a group needs is asked for before any of it is used.
 template <int DT, int SG>
 __global__ __launch_bounds__(256) void paged_combine_kernel(PagedAttn a) {
-  constexpr int TB = SG == 1 ? 2 : 8;             // units at a time
+  constexpr int TB = SG == 1 ? 2 : 8;                  // units at a time
   constexpr int TN = SG == 1 && DT == PT_F32 ? 4 : 8;  // nodes at a time
-  using Quad = typename QuadOf<DT>::type;
   __shared__ float4 so[SG > 1 ? 256 : 1];
   __shared__ float2 sml[SG > 1 ? 256 : 1];
   const int dh = a.pool.dh, quads = dh / 4, heads = 256 / SG / quads;  // heads of a workgroup
@@ -866,27 +685,18 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(PagedAttn a) {
   const int grp = SG == 1 ? 0 : threadIdx.x / (256 / SG), t = SG == 1 ? threadIdx.x : threadIdx.x % (256 / SG);
   const int h = min((int)blockIdx.y * heads + t / quads, a.Hq - 1), d = t % quads * 4, hk = h / G;
   const bool mine = blockIdx.y * heads + t / quads < a.Hq;
-  uint64_t anc = anc_of(a, b, i);
+  const uint64_t anc = anc_of(a, b, i);
   const int2 un = a.units > 0 ? a.first_unit[b] : make_int2(0, 0);
   bool bad = false;
   const int len = checked_len(a.tab, b, &bad);
   int count = a.counts ? a.counts[b] : a.nodes;
-  const long long qo = b * a.q.sb + i * a.q.sr + h * a.q.sh + d;
-  float4 q;
-  if (DT == PT_F32 && a.q_lo.p) {
-    q = quad_f32<PT_BF16>(load_quad<PT_BF16>(a.q.p, qo, a.q.vec));
-    const float4 y = quad_f32<PT_BF16>(load_quad<PT_BF16>(a.q_lo.p, qo, a.q.vec));
-    q.x += y.x, q.y += y.y, q.z += y.z, q.w += y.w;
-  } else {
-    q = quad_f32<DT>(load_quad<DT>(a.q.p, qo, a.q.vec));
-  }
+  const float4 q = query_quad<DT>(a, b * a.q.sb + i * a.q.sr + h * a.q.sh + d);
   if (count < 0 || count > a.nodes) bad = true, count = min(max(count, 0), a.nodes);
   if (bad && a.status && threadIdx.x == 0) atomicOr(a.status, PAGED_BAD_LENGTH);
   const bool live = i < count;
   if (!live && a.out_ks == 0) return;  // uniform
   float4 out = make_float4(0.f, 0.f, 0.f, 0.f);
   if (live) {
-    const int dep = depth_of(anc, i);
     float m = -INFINITY, l = 0.f;
     float4 o = out;
     // a sequence without tiles has no units (and nobody wrote their place)
@@ -904,26 +714,9 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(PagedAttn a) {
           ou[x] = *reinterpret_cast<const float4*>(a.part_o + at * dh + d);
         }
     };
-    const long long kb = b * a.k.sb + hk * a.k.sh + d, vb = b * a.v.sb + hk * a.v.sh + d;
-    if (grp != SG - 1) anc = 0;
-    int r = 0, seen = 0;  // rank of the next node, the batch's seen ones
-    Quad k4[TN], v4[TN];
-    auto ask_nodes = [&]() {
-      seen = 0;
-#pragma unroll
-      for (int x = 0; x < TN; ++x) {
-        if (!anc) break;  // uniform
-        const int j = __builtin_ctzll(anc);
-        anc &= anc - 1;
-        if (!a.cut.window || dep - r < a.cut.window || (long long)len + r < a.cut.sinks) seen |= 1 << x;
-        ++r;
-        k4[x] = load_quad<DT>(a.k.p, kb + j * a.k.sr, a.k.vec);
-        v4[x] = load_quad<DT>(a.v.p, vb + j * a.v.sr, a.v.vec);
-      }
-    };
+    RootPath<DT, TN> path;
     ask(grp);
-    const uint64_t path = anc;
-    ask_nodes();
+    path.start(a, b, hk, d, grp == SG - 1 ? anc : 0, depth_of(anc, i), len);
     for (int s = grp; s < units; s += TB * SG) {
       if (s != grp) ask(s);
       float mn = m;
@@ -943,41 +736,7 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(PagedAttn a) {
         }
       m = mn;
     }
-    // nodes of the root path
-    for (bool any = path != 0; any;) {
-      if (seen) {
-        float sc[TN];
-#pragma unroll
-        for (int x = 0; x < TN; ++x) {
-          sc[x] = 0.f;
-          if (seen >> x & 1) {
-            const float4 k = quad_f32<DT>(k4[x]);
-            sc[x] = q.x * k.x + q.y * k.y + q.z * k.z + q.w * k.w;
-          }
-        }
-        for (int s = quads >> 1; s > 0; s >>= 1)
-#pragma unroll
-          for (int x = 0; x < TN; ++x) sc[x] += __shfl_xor(sc[x], s, 64);
-        float mn = m;
-#pragma unroll
-        for (int x = 0; x < TN; ++x)
-          if (seen >> x & 1) mn = fmaxf(mn, sc[x] *= a.scale_log2);
-        const float al = m == -INFINITY ? 0.f : exp2f(m - mn);
-        l *= al;
-        o.x *= al, o.y *= al, o.z *= al, o.w *= al;
-#pragma unroll
-        for (int x = 0; x < TN; ++x)
-          if (seen >> x & 1) {
-            const float e = exp2f(sc[x] - mn);
-            const float4 v = quad_f32<DT>(v4[x]);
-            l += e;
-            o.x += e * v.x, o.y += e * v.y, o.z += e * v.z, o.w += e * v.w;
-          }
-        m = mn;
-      }
-      any = anc != 0;
-      if (any) ask_nodes();
-    }
+    path.add(a, q, quads, m, l, o);
     if constexpr (SG > 1) {
       so[threadIdx.x] = o;
       sml[threadIdx.x] = make_float2(m, l);
@@ -999,35 +758,9 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(PagedAttn a) {
         }
       }
     }
-    const float inv = l == 0.f ? 0.f : 1.f / l;  // a row that sees nothing is 0
-    out = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
-    if (bad) out.x = out.y = out.z = out.w = __builtin_nanf("");
+    out = row_output(l, o, bad);
   }
-  if (grp != 0 || !mine) return;
-  if (a.out_ks) {
-    uint16_t* dst = static_cast<uint16_t*>(a.out) + xpack_off((long long)b * a.nodes + i, h * dh + d, a.out_ks);
-    const Hilo2 p0 = pack_hilo2(out.x, out.y), p1 = pack_hilo2(out.z, out.w);
-    *reinterpret_cast<uint2*>(dst) = make_uint2(p0.hi, p1.hi);
-    *reinterpret_cast<uint2*>(dst + XPACK_LO) = make_uint2(p0.lo, p1.lo);
-    return;
-  }
-  const long long at = b * a.ob + i * a.orow + h * a.oh + d;
-  if constexpr (DT == PT_F32) {
-    float* f = static_cast<float*>(a.out) + at;
-    if (a.out_vec) *reinterpret_cast<float4*>(f) = out;
-    else f[0] = out.x, f[1] = out.y, f[2] = out.z, f[3] = out.w;
-  } else {
-    uint2 w;
-    if constexpr (DT == PT_BF16) {
-      w = make_uint2(pack_bf16x2(out.x, out.y), pack_bf16x2(out.z, out.w));
-    } else {
-      const f16x2 x = __builtin_convertvector(f32x2{out.x, out.y}, f16x2), y = __builtin_convertvector(f32x2{out.z, out.w}, f16x2);
-      w = make_uint2(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, y));
-    }
-    uint16_t* p = static_cast<uint16_t*>(a.out) + at;
-    if (a.out_vec) *reinterpret_cast<uint2*>(p) = w;
-    else p[0] = w.x, p[1] = w.x >> 16, p[2] = w.y, p[3] = w.y >> 16;
-  }
+  if (grp == 0 && mine) store_row<DT>(a, b, i, h, d, out);
 }
 
 }  // namespace
@@ -1039,18 +772,26 @@ int paged_plan(PagedAttn& a, int max_length) {
   if (a.cut.window)
     most = std::min(most, ((long long)a.cut.window + 30) / 32 + 1 + ((long long)a.cut.sinks + 31) / 32);
   if (most * a.batch > 0x7fffffffLL) return -1;
+  a.thin = R <= 16;
+  // One workgroup per sequence and KV head, which reads about 100 GB/s: up to 72
+  // tiles while that leaves half of the CUs idle (a token over 2077 slots 12.5
+  // us against 7 + 5 and a second launch, over 4096 18 against 7 + 5), else up
+  // to 160 (16 chains over up to 2048 slots 14 us against 13 + 5, 16 tokens with
+  // a window of 4096 28 against 26 + 5).
+  a.fused = a.thin && most <= ((long long)a.batch * a.pool.Hkv < 128 ? 72 : 160);
   // The wide kernel where a KV head has more than two row tiles and its units
   // are long: at least 32 tiles for each of the 256 workgroups that then fill
   // the chip.
   const int nw = R > 128 ? 8 : 4, wide_blocks = (R + 32 * nw - 1) / (32 * nw);
   a.wide = R > 64 && a.batch * most * a.pool.Hkv * wide_blocks >= 32 * 256 ? nw : 0;
   const int streams = a.pool.Hkv * (a.wide ? wide_blocks : (R + 31) / 32);
-  a.cut.target = std::max(1, (a.wide == 8 ? 256 : 512) / streams);
+  // workgroups that fit the 256 CUs at once
+  a.cut.target = std::max(1, (a.thin ? 1024 : a.wide == 8 ? 256 : 512) / streams);
   a.cut.least = 8;
-  a.cut.full = a.wide ? 0 : 32;
+  a.cut.full = a.wide ? 0 : a.thin ? 64 : 32;
   // units of a sequence of n tiles: ceil(n / per) with per >= least and >= all tiles / target
   const long long by_len = (long long)a.batch * ((most + a.cut.least - 1) / a.cut.least);
-  a.units = (int)std::min<long long>(by_len, (long long)a.cut.target + a.batch);
+  a.units = a.fused ? 0 : (int)std::min<long long>(by_len, (long long)a.cut.target + a.batch);
   return 0;
 }
 
@@ -1086,7 +827,10 @@ static void launch_combine(const PagedAttn& a, bool few, hipStream_t s) {
 hipError_t launch_paged_attention(const PagedAttn& a, hipStream_t s) {
   const int R = a.Hq / a.pool.Hkv * a.nodes, rows = a.wide ? 32 * a.wide : 32;
   if (a.pool.dh != 64 && a.pool.dh != 128) return hipErrorInvalidValue;
-  if (a.units > 0) {
+  if (a.thin && (a.fused || a.units > 0)) {
+    const hipError_t e = launch_paged_thin(a, s);
+    if (e != hipSuccess || a.fused) return e;
+  } else if (a.units > 0) {
     const long long wgs = ((long long)a.units * a.pool.Hkv + 7) / 8 * 8 * ((R + rows - 1) / rows);
     if (wgs > 0x7fffffffLL) return hipErrorInvalidValue;
     if (a.pool.dh == 128) launch_form<128>(a, dim3((unsigned)wgs), s);

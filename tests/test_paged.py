@@ -129,10 +129,11 @@ def test_attention_refuses(code, kw):
 
 def test_attention_wants_its_workspace():
     N = _lib()
-    args = attention_args(most=100)
+    # 5 nodes of 4 heads on each of 2 key heads: 20 rows, which units share
+    args = attention_args(most=100, nodes=5, hq=8)
     need = N.lib.griffin_paged_attention_workspace(args)
-    # one unit of at most eight tiles of 32 slots: 8 rows of 128 outputs and 2 sums, and the unit's place
-    assert need == 8 * 130 * 4 + 8
+    # one unit of at most eight tiles of 32 slots: 40 rows of 128 outputs and 2 sums, and the unit's place
+    assert need == 40 * 130 * 4 + 8
     assert N.lib.griffin_paged_attention(args, 256, need - 1, None) == N.CODES["GRIFFIN_ENOMEM"]
     assert N.lib.griffin_paged_attention(args, 0, need, None) == N.CODES["GRIFFIN_EINVAL"]
     assert N.lib.griffin_paged_attention(args, 264, need, None) == N.CODES["GRIFFIN_EINVAL"]

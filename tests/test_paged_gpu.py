@@ -312,6 +312,16 @@ def test_ragged_batches(G):
     run_case(G, 2, 64, 32, lengths, 3, "f32", hq=2, counts=counts, max_length=2000)
 
 
+@pytest.mark.parametrize("dtype,dh,nodes,hq", [("bf16", 128, 1, 8), ("bf16", 64, 4, 4), ("f16", 128, 3, 10), ("f32", 128, 2, 16),
+                                               ("f32", 64, 16, 2), ("f16", 64, 5, 6)])
+@pytest.mark.parametrize("window", [0, 900])
+def test_few_rows_in_units(G, dtype, dh, nodes, hq, window):
+    """At most 16 rows a key head over sequences that are cut into units: the
+    bound of the lengths asks for it, the lengths go from none to many tiles."""
+    run_case(G, 2, dh, 64, [0, 8, 2049, 5000, 333], nodes, dtype, hq=hq, counts=[nodes, 1, nodes, max(1, nodes - 1), 0],
+             window=window, sinks=40 if window else 0, max_length=5056)
+
+
 def test_more_sequences_than_lanes(G):
     rng = np.random.default_rng(1)
     run_case(G, 1, 64, 32, [int(x) for x in rng.integers(0, 90, 130)], 1, "f16", hq=4)
