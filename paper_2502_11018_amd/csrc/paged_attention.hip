@@ -23,9 +23,8 @@
 //    fp16 inputs); fp32 inputs enter as high and low parts (22 bits), and so
 //    do their probabilities.  The others' probabilities are rounded to fp16,
 //    2^-12 relative: an eighth of the rounding of a bf16 output.
-//  * The maximum that the probabilities refer to follows the scores only where
-//    a lane's sum of a tile passes 2^14 (fp16 ends at 65504), so no maximum is
-//    formed for most tiles.
+//  * What the probabilities refer to follows the scores only where a lane's sum
+//    of a tile passes 2^P_TOP, so no maximum is formed for most tiles.
 //
 // paged_combine_kernel joins a row's units in their order, adds the nodes of
 // its own root path in fp32, and writes the row.
@@ -57,6 +56,16 @@ struct Query {
   i32x8 e[QF == Q_FP8 ? KP / 2 : 1][2];
   float fac;  // the scores' scale in the log2 domain, and the power of two that the row was scaled by
 
+  __device__ __forceinline__ void take(const SplitRows<DH, 32>& rows, int col, int hh) {
+    fac = rows.fac[col];
+#pragma unroll
+    for (int x = 0; x < KP; ++x)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        a[x][h] = rows.get(0, col, 4 * x + 2 * hh + h);
+        b[x][h] = rows.get(1, col, 4 * x + 2 * hh + h);
+      }
+  }
   __device__ __forceinline__ void load(const PagedAttn& p, long long at) {
     fac = p.scale_log2;
     if constexpr (QF == Q_BF16 || QF == Q_F16) {
@@ -65,22 +74,7 @@ struct Query {
 #pragma unroll
         for (int h = 0; h < 2; ++h) a[x][h] = load8_raw(p.q.p, at + 32 * x + 8 * h, p.q.vec);
     } else {
-      float v[KP][2][8];
-      float mx = 0.f;
-#pragma unroll
-      for (int x = 0; x < KP; ++x)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          load8(p.q.p, at + 32 * x + 8 * h, QF == Q_FP8 || p.q_lo.p ? PT_BF16 : PT_F32, p.q.vec, v[x][h]);
-          if (QF == Q_SPLIT && p.q_lo.p) {
-            float y[8];
-            load8(p.q_lo.p, at + 32 * x + 8 * h, PT_BF16, p.q.vec, y);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[x][h][i] += y[i];
-          }
-#pragma unroll
-          for (int i = 0; i < 8; ++i) mx = fmaxf(mx, fabsf(v[x][h][i]));
-        }
+      float v[KP][2][8], mx = load_query<KP, 2, 32, QF == Q_SPLIT>(p, at, v);
       mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
       constexpr int TOP = QF == Q_FP8 ? 7 : 8;  // the row's largest value to [2^TOP, 2^(TOP + 1))
       const int ex = scale_exponent(mx);
@@ -157,7 +151,7 @@ struct Query {
 };
 
 // Running softmax and output of a row tile: lane col's row (both halves hold
-// it), dims 32 d + 8 (r / 4) + 4 hh + r % 4 of it in o[d][r], times 2^-E.
+// it), dims 32 d + 8 (r / 4) + 4 hh + r % 4 of it in o[d][r], times 2^(V_LIFT - E).
 template <int DH>
 struct State {
   float m, l;
@@ -175,13 +169,13 @@ struct State {
 #pragma unroll
     for (int d = 0; d < DH / 32; ++d) o[d] *= f;
   }
-  // raise the reference to the scores' maximum (both halves')
+  // raise the reference towards the scores' maximum (both halves')
   __device__ __forceinline__ void follow(const f32x16& s, float f) {
     float mx = -INFINITY;
 #pragma unroll
     for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[r]);
     mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * f;
-    const float mn = fmaxf(m, mx), al = __builtin_amdgcn_exp2f(m - mn);
+    const float mn = fmaxf(m, mx - P_LIFT), al = __builtin_amdgcn_exp2f(m - mn);
     m = mn;
     l *= al;
     scale(al);
@@ -222,13 +216,13 @@ __device__ __forceinline__ void attend(State<DH>& st, f32x16 s, Vals<DH> v, floa
     sum = x[0];
   };
   probs();
-  if (__any(sum > 16384.f)) {
+  if (__any(sum > pow2i(P_TOP))) {
     st.follow(s, f);
     probs();
   }
   st.l += sum;
   st.reach(ve);
-  const float vs = pow2i(ve - st.E);
+  const float vs = value_factor(ve, st.E);
   if constexpr (EDGE::value) {
     // what lies in slots that a row does not see must not reach it, NaN
     // included: bytes that no row sees become 0 ..
@@ -315,7 +309,7 @@ __device__ __forceinline__ void load_vals(const PagedAttn& a, long long at, int 
 template <int DH>
 __device__ __forceinline__ void put_rows(const State<DH>& st, int col, int hh, int rows, float* buf) {
   if (col >= rows) return;
-  const float fe = pow2i(st.E);
+  const float fe = out_factor(st.E);
 #pragma unroll
   for (int d = 0; d < DH / 32; ++d)
 #pragma unroll
@@ -327,12 +321,14 @@ __device__ __forceinline__ void put_rows(const State<DH>& st, int col, int hh, i
 }
 
 // One row tile per workgroup, whose four waves take every fourth tile of the
-// unit each and meet in LDS.  Two workgroups per CU; the next tile's loads are
-// in flight while one is computed.
+// unit each and meet in LDS; two workgroups per CU, the next tile's loads in
+// flight while one is computed.  (One workgroup of eight waves for a whole
+// sequence, with the join, is slower down to 200 slots: 61 nodes 14.8 us against
+// 9.4 + 5.4.)
 template <int DH, int QF>
 __global__ __launch_bounds__(256, 2) void paged_attention_kernel(PagedAttn a) {
   constexpr int NW = 4;
-  __shared__ float so[NW][32 * DH];
+  __shared__ __align__(16) float so[NW][32 * DH];
   __shared__ float sm[NW][32], sl[NW][32];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 31, hh = lane >> 5;
@@ -341,7 +337,7 @@ __global__ __launch_bounds__(256, 2) void paged_attention_kernel(PagedAttn a) {
   if (!place_of(a, (R + 31) / 32, p)) return;
   const int count = a.counts ? a.counts[p.b] : a.nodes;
 
-  // lane j looks up the j-th of 64 of the wave's tiles i0 + w, i0 + w + 4, ..
+  // lane j looks up the j-th of 64 of the wave's tiles i0 + w, i0 + w + NW, ..
   const int mine = p.i1 - p.i0 - w > 0 ? (p.i1 - p.i0 - w + NW - 1) / NW : 0;
   int my_tile = 0, my_at = 0, my_ke = 0, my_ve = 0;
   auto look = [&](int base) {
@@ -354,10 +350,17 @@ __global__ __launch_bounds__(256, 2) void paged_attention_kernel(PagedAttn a) {
     }
   };
   look(0);
-  const int row = min(p.rb * 32 + col, R - 1), node = row % a.nodes, hq = p.hk * G + row / a.nodes;
+  const int node = min(p.rb * 32 + col, R - 1) % a.nodes;
   const int pos = a.cut.window ? p.sight.len + depth_of(anc_of(a, p.b, node), node) : 0;
   Query<DH, QF> q;
-  q.load(a, p.b * a.q.sb + node * a.q.sr + hq * a.q.sh + 16 * hh);
+  if constexpr (QF == Q_SPLIT) {
+    auto& rows = *reinterpret_cast<SplitRows<DH, 32>*>(so);
+    static_assert(sizeof(rows) <= sizeof(so));
+    rows.fill(a, [&](int r) { return query_row(a, p, p.rb * 32 + r); });
+    q.take(rows, col, hh);
+  } else {
+    q.load(a, query_row(a, p, p.rb * 32 + col) + 16 * hh);
+  }
   State<DH> st;
   st.clear();
   for (int base = 0; base < mine; base += 64) {
@@ -407,31 +410,32 @@ __global__ __launch_bounds__(256, 2) void paged_attention_kernel(PagedAttn a) {
       if (--left == 0) break;
     }
   }
+  if constexpr (QF == Q_SPLIT) __syncthreads();  // every wave has its queries
   float l = st.l + __shfl_xor(st.l, 32, 64);
   if (__any(p.bad)) l = __builtin_nanf("");  // a tile that is not there: the rows become NaN
   put_rows<DH>(st, col, hh, R - p.rb * 32, so[w]);
-  if (hh == 0) sm[w][col] = st.m, sl[w][col] = l;
+  const float2 ml = out_sums(st.m, l);
+  if (hh == 0) sm[w][col] = ml.x, sl[w][col] = ml.y;
   __syncthreads();
   constexpr int CH = DH / 4;
   const long long prow = ((long long)p.u * a.pool.Hkv + p.hk) * R + p.rb * 32;
-  const int live = min(32, R - p.rb * 32);
-  for (int i = threadIdx.x; i < live * CH; i += 256) {
-    const int r = i / CH, c = i % CH;
-    if (count < a.nodes && (p.rb * 32 + r) % a.nodes >= count) continue;  // an absent node
-    float M = sm[0][r];
+  for (int i = threadIdx.x; i < 32 * CH; i += 256) {
+    const int r = i / CH, c = i % CH, gr = p.rb * 32 + r;
+    if (gr >= R || (count < a.nodes && gr % a.nodes >= count)) continue;  // an absent node
+    float m = sm[0][r];
 #pragma unroll
-    for (int x = 1; x < NW; ++x) M = fmaxf(M, sm[x][r]);
+    for (int x = 1; x < NW; ++x) m = fmaxf(m, sm[x][r]);
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
     float L = 0.f;
 #pragma unroll
     for (int x = 0; x < NW; ++x) {
-      const float f = __builtin_amdgcn_exp2f(sm[x][r] - M);
+      const float f = __builtin_amdgcn_exp2f(sm[x][r] - m);
       const float4 v = *reinterpret_cast<const float4*>(&so[x][r * DH + 4 * (c ^ (r & 7))]);
       o.x += f * v.x, o.y += f * v.y, o.z += f * v.z, o.w += f * v.w;
       L += f * sl[x][r];
     }
     *reinterpret_cast<float4*>(a.part_o + (prow + r) * DH + 4 * c) = o;
-    if (c == 0) *reinterpret_cast<float2*>(a.part_ml + (prow + r) * 2) = make_float2(M, L);
+    if (c == 0) *reinterpret_cast<float2*>(a.part_ml + (prow + r) * 2) = make_float2(m, L);
   }
 }
 
@@ -552,7 +556,7 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_wide_kernel(PagedAttn a) {
     // a tile's factor of the scores, and whether its scores or its values'
     // exponent go beyond what the state refers to
     auto factor = [&](int ex) { return fmaxf(q.fac * __int_as_float(ex & 0x7f800000), 0x1p-126f); };
-    auto beyond = [&](float mx, float f, int ex) { return __any(fmaf(mx, f, -st.m) > 14.f) || (int8_t)ex > st.E; };
+    auto beyond = [&](float mx, float f, int ex) { return __any(fmaf(mx, f, -st.m) > P_TOP) || (int8_t)ex > st.E; };
     f32x16 sa, sb;
     wait_vmcnt_lds<(D - 4) * PPW>();  // pairs 0 and 1
     __builtin_amdgcn_s_barrier();
@@ -575,7 +579,7 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_wide_kernel(PagedAttn a) {
         st.follow(s, f);
         st.reach((int8_t)ex);
       }
-      const float vs = pow2i((int8_t)ex - st.E);
+      const float vs = value_factor((int8_t)ex, st.E);
       const int s1 = slot + 1 == D ? 0 : slot + 1, s2 = s1 + 1 == D ? 0 : s1 + 1;
       const int exn = of(ex0, ex1, min(i + 1, whole - 1));
       const float fn = factor(exn);
@@ -659,7 +663,7 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_wide_kernel(PagedAttn a) {
   if (hurt) l = __builtin_nanf("");
   put_rows<DH>(st, col, hh, R - row0, buf);
   auto live = [&](int r) { return row0 + r < R && (count >= a.nodes || (row0 + r) % a.nodes < count); };
-  if (hh == 0 && live(col)) *reinterpret_cast<float2*>(a.part_ml + (prow + col) * 2) = make_float2(st.m, l);
+  if (hh == 0 && live(col)) *reinterpret_cast<float2*>(a.part_ml + (prow + col) * 2) = out_sums(st.m, l);
 #pragma unroll 4
   for (int n = 0; n < 32 / RPI; ++n) {
     const int r = n * RPI + lane / CH, c = lane % CH;
@@ -765,6 +769,8 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(PagedAttn a) {
 
 }  // namespace
 
+constexpr int UNIT_LEAST = 8;  // tiles: two for each of a workgroup's four waves
+
 int paged_plan(PagedAttn& a, int max_length) {
   const int R = a.Hq / a.pool.Hkv * a.nodes;
   // tiles of a sequence: all, or those that window - 1 slots can touch and the sinks
@@ -772,25 +778,30 @@ int paged_plan(PagedAttn& a, int max_length) {
   if (a.cut.window)
     most = std::min(most, ((long long)a.cut.window + 30) / 32 + 1 + ((long long)a.cut.sinks + 31) / 32);
   if (most * a.batch > 0x7fffffffLL) return -1;
-  a.thin = R <= 16;
-  // One workgroup per sequence and KV head, which reads about 100 GB/s: up to 72
-  // tiles while that leaves half of the CUs idle (a token over 2077 slots 12.5
-  // us against 7 + 5 and a second launch, over 4096 18 against 7 + 5), else up
-  // to 160 (16 chains over up to 2048 slots 14 us against 13 + 5, 16 tokens with
-  // a window of 4096 28 against 26 + 5).
-  a.fused = a.thin && most <= ((long long)a.batch * a.pool.Hkv < 128 ? 72 : 160);
   // The wide kernel where a KV head has more than two row tiles and its units
   // are long: at least 32 tiles for each of the 256 workgroups that then fill
   // the chip.
-  const int nw = R > 128 ? 8 : 4, wide_blocks = (R + 32 * nw - 1) / (32 * nw);
+  const int nw = R > 128 ? 8 : 4, wide_blocks = (R + 32 * nw - 1) / (32 * nw), thin_blocks = (R + 15) / 16;
   a.wide = R > 64 && a.batch * most * a.pool.Hkv * wide_blocks >= 32 * 256 ? nw : 0;
-  const int streams = a.pool.Hkv * (a.wide ? wide_blocks : (R + 31) / 32);
+  // Row tiles of 16 where one holds all rows, and where all workgroups fit the
+  // chip at once, as a wave then has half of the work: 61 nodes of 4 heads over
+  // 500 slots 8 us against 10 (512 workgroups), over 2048 slots 13 against 12
+  // (1152), of 1 head in fp32 over 1024 slots 17 against 20 (512).
+  const long long by_len = (long long)a.batch * ((most + UNIT_LEAST - 1) / UNIT_LEAST);
+  a.thin = R <= 16 || by_len * a.pool.Hkv * thin_blocks <= 1024;
+  // One workgroup of eight waves for all of a (sequence, KV head), which reads
+  // about 100 GB/s: up to 72 tiles while that leaves half of the CUs idle (a token
+  // over 2077 slots 12.5 us against 7 + 5 and a second launch, over 4096 18
+  // against 7 + 5), else up to 160 (16 chains over up to 2048 slots 14 us against
+  // 13 + 5, 16 tokens with a window of 4096 28 against 26 + 5).
+  const long long wgs = (long long)a.batch * a.pool.Hkv;
+  a.fused = R <= 16 && wgs < (1 << 30) && most <= (wgs < 128 ? 72 : 160);
+  const int streams = a.pool.Hkv * (a.wide ? wide_blocks : a.thin ? thin_blocks : (R + 31) / 32);
   // workgroups that fit the 256 CUs at once
   a.cut.target = std::max(1, (a.thin ? 1024 : a.wide == 8 ? 256 : 512) / streams);
-  a.cut.least = 8;
+  a.cut.least = UNIT_LEAST;
   a.cut.full = a.wide ? 0 : a.thin ? 64 : 32;
   // units of a sequence of n tiles: ceil(n / per) with per >= least and >= all tiles / target
-  const long long by_len = (long long)a.batch * ((most + a.cut.least - 1) / a.cut.least);
   a.units = a.fused ? 0 : (int)std::min<long long>(by_len, (long long)a.cut.target + a.batch);
   return 0;
 }

@@ -4,6 +4,8 @@
 #pragma once
 
 #include "griffin_internal.h"
+#include <type_traits>
+
 #include "paged.h"
 
 namespace griffin {
@@ -107,6 +109,19 @@ __device__ __forceinline__ uint64_t anc_of(const PagedAttn& a, int b, int i) {
 __device__ __forceinline__ int depth_of(uint64_t anc, int i) { return __builtin_popcountll(anc & ~(1ull << i)); }
 
 constexpr float NO_MAX = -3e38f;  // reference of a row that has seen no key
+// fp16 holds steps of 2^-24 and ends at 2^16.  A row's largest probability
+// stands at 2^P_LIFT or above and follows the scores up to 2^P_TOP, so that what
+// is rounded away is at most 2^-(25 + P_LIFT) of it: a lift of 10 made references
+// rise more often (8 x 61 nodes over 16384 slots 145 us against 142), one of 0
+// loses many small weights beside a large one.  Values of the largest exponent
+// met, E, stand at 2^V_LIFT times their bytes (at most 448): bytes are multiples
+// of 2^-9, so that tiles down to E - 21 are exact.
+constexpr int P_LIFT = 8, P_TOP = 15, V_LIFT = 6;
+static_assert(PAGED_E_MIN - V_LIFT - P_LIFT >= -126, "pow2i");
+__device__ __forceinline__ float value_factor(int ve, int E) { return pow2i(ve - E + V_LIFT); }
+// A wave's result for the join: the lifts taken out
+__device__ __forceinline__ float out_factor(int E) { return pow2i(E - V_LIFT - P_LIFT); }
+__device__ __forceinline__ float2 out_sums(float m, float l) { return make_float2(m + P_LIFT, l * pow2i(-P_LIFT)); }
 
 // How q enters the matrix cores, by its type and the kernel:
 //   Q_BF16   bf16 as it is, keys converted to bf16
@@ -125,12 +140,101 @@ __device__ __forceinline__ int scale_exponent(float mx) {
   return min(max((int)(__float_as_uint(mx) >> 23) - 127, -110), 118);
 }
 
+// Dims at + STEP x + 8 h .. of a query row, bf16 (with SPLIT: plus its low part, or
+// fp32).  One block per type and alignment, so that all loads are in flight at
+// once.  Returns the largest magnitude.
+template <int NX, int NH, int STEP, bool SPLIT>
+__device__ __forceinline__ float load_query(const PagedAttn& p, long long at, float (&v)[NX][NH][8]) {
+  if (!SPLIT || p.q_lo.p) {
+    auto rows = [&](const void* q, auto vec, u32x4(&w)[NX][NH]) {
+#pragma unroll
+      for (int x = 0; x < NX; ++x)
+#pragma unroll
+        for (int h = 0; h < NH; ++h) w[x][h] = load8_raw(q, at + STEP * x + 8 * h, decltype(vec)::value);
+    };
+    u32x4 w[NX][NH], y[SPLIT ? NX : 1][NH];
+    if (p.q.vec) {
+      rows(p.q.p, std::true_type{}, w);
+      if constexpr (SPLIT) rows(p.q_lo.p, std::true_type{}, y);
+    } else {
+      rows(p.q.p, std::false_type{}, w);
+      if constexpr (SPLIT) rows(p.q_lo.p, std::false_type{}, y);
+    }
+#pragma unroll
+    for (int x = 0; x < NX; ++x)
+#pragma unroll
+      for (int h = 0; h < NH; ++h)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          v[x][h][i] = bf16_to_f32((uint16_t)(w[x][h][i / 2] >> (16 * (i & 1))));
+          if constexpr (SPLIT) v[x][h][i] += bf16_to_f32((uint16_t)(y[x][h][i / 2] >> (16 * (i & 1))));
+        }
+  } else {
+    const float* f = static_cast<const float*>(p.q.p) + at;
+    auto rows = [&](auto vec) {
+#pragma unroll
+      for (int x = 0; x < NX; ++x)
+#pragma unroll
+        for (int h = 0; h < NH; ++h) load8(f, STEP * x + 8 * h, PT_F32, decltype(vec)::value, v[x][h]);
+    };
+    if (p.q.vec) rows(std::true_type{});
+    else rows(std::false_type{});
+  }
+  float mx = 0.f;
+#pragma unroll
+  for (int x = 0; x < NX; ++x)
+#pragma unroll
+    for (int h = 0; h < NH; ++h)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) mx = fmaxf(mx, fabsf(v[x][h][i]));
+  return mx;
+}
+
 // Two values as fp16 high and low parts (22 bits)
 __device__ __forceinline__ Hilo2 split_f16(float x, float y) {
   const f16x2 h = __builtin_convertvector(f32x2{x, y}, f16x2);
   const f16x2 l = __builtin_convertvector(f32x2{x - (float)h.x, y - (float)h.y}, f16x2);
   return {__builtin_bit_cast(uint32_t, h), __builtin_bit_cast(uint32_t, l)};
 }
+
+// A row tile's queries in two fp16 parts, as the waves of a workgroup share
+// them: a thread takes 8 dims of a row, so that whole rows are read together and
+// split once.  (In the operands' order each wave's loads touch every line of the
+// fp32 rows many times: 61 nodes of 32 heads over 1024 slots 17 us against 12.
+// 16-bit rows, which are operands as they stand, are read so: 0.5 us less than
+// through LDS.)  Chunk c of row r stands at c ^ r.
+template <int DH, int ROWS>
+struct SplitRows {
+  static constexpr int CQ = DH / 8;
+  u32x4 part[2][ROWS][CQ];
+  float fac[ROWS];  // the scores' scale in the log2 domain, and the power of two that a row was scaled by
+
+  // by all threads; at(r): where row r starts.  Ends with a barrier.
+  template <class At>
+  __device__ __forceinline__ void fill(const PagedAttn& a, At at) {
+    for (int i = threadIdx.x; i < ROWS * CQ; i += blockDim.x) {
+      const int r = i / CQ, c = i % CQ, put = c ^ (r % CQ);
+      float v[1][1][8];
+      float mx = load_query<1, 1, 0, true>(a, at(r) + 8 * c, v);
+#pragma unroll
+      for (int s = CQ / 2; s > 0; s >>= 1) mx = fmaxf(mx, __shfl_xor(mx, s, 64));
+      const int ex = scale_exponent(mx);
+      const float f = pow2i(8 - ex);  // the row's largest value to [2^8, 2^9)
+      u32x4 hi, lo;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const Hilo2 x = split_f16(v[0][0][2 * e] * f, v[0][0][2 * e + 1] * f);
+        hi[e] = x.hi;
+        lo[e] = x.lo;
+      }
+      part[0][r][put] = hi;
+      part[1][r][put] = lo;
+      if (c == 0) fac[r] = a.scale_log2 * pow2i(ex - 8);
+    }
+    __syncthreads();
+  }
+  __device__ __forceinline__ u32x4 get(int x, int r, int c) const { return part[x][r][c ^ (r % CQ)]; }
+};
 
 // A score's factor on a tile: never 0, which times a masked -inf would be a NaN.
 __device__ __forceinline__ float score_factor(float fac, int ke) { return fmaxf(fac * pow2i(ke), 0x1p-126f); }
@@ -158,14 +262,37 @@ struct Place {
   Sight sight;
   bool bad;
 };
-__device__ __forceinline__ bool place_of(const PagedAttn& a, int blocks, Place& p) {
-  // XCD-aware decode: workgroups go round-robin over the 8 XCDs, so the row
-  // blocks of one (unit, KV head) get the same id % 8 and share its L2
+// XCD-aware decode of the workgroup's number: workgroups go round-robin over
+// the 8 XCDs, so the row blocks of one (unit or sequence, KV head) get the same
+// id % 8 and share its L2.
+__device__ __forceinline__ int decode_group(const PagedAttn& a, int blocks, Place& p) {
   const int id = blockIdx.x, rest = id >> 3;
   p.rb = rest % blocks;
   const int st = (rest / blocks) * 8 + (id & 7);
   p.hk = st % a.pool.Hkv;
-  p.u = st / a.pool.Hkv;
+  return st / a.pool.Hkv;
+}
+// Where row `row` of the KV head's starts in q (behind the last one: that again)
+__device__ __forceinline__ long long query_row(const PagedAttn& a, const Place& p, int row) {
+  const int G = a.Hq / a.pool.Hkv;
+  row = min(row, G * a.nodes - 1);
+  return p.b * a.q.sb + row % a.nodes * a.q.sr + (p.hk * G + row / a.nodes) * a.q.sh;
+}
+// All of a sequence; false: none (the grid is rounded up).
+__device__ __forceinline__ bool whole_sequence(const PagedAttn& a, int blocks, Place& p) {
+  p.b = decode_group(a, blocks, p);
+  if (p.b >= a.batch) return false;  // uniform
+  p.u = 0;
+  p.bad = false;
+  const int len = checked_len(a.tab, p.b, &p.bad);
+  p.seq = seq_tiles(len, a.cut);
+  p.i0 = 0;
+  p.i1 = p.seq.n;
+  p.sight = Sight{len, a.cut.window, a.cut.sinks};
+  return true;
+}
+__device__ __forceinline__ bool place_of(const PagedAttn& a, int blocks, Place& p) {
+  p.u = decode_group(a, blocks, p);
   const UnitAt at = unit_at(a, p.u);
   if (at.b < 0) return false;  // uniform
   p.b = at.b;

@@ -50,47 +50,22 @@ struct ThinQuery {
   u32x4 a[J][2], b[QF == Q_SPLIT ? J : 1][2];
   float fac;
 
-  __device__ __forceinline__ void load(const PagedAttn& p, long long at, int g) {
+  __device__ __forceinline__ void load(const PagedAttn& p, long long at, int g) {  // the row starts at `at`
     fac = p.scale_log2;
-    at += 16 * g;
-    if constexpr (QF != Q_SPLIT) {
 #pragma unroll
-      for (int j = 0; j < J; ++j)
+    for (int j = 0; j < J; ++j)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) a[j][h] = load8_raw(p.q.p, at + 64 * j + 8 * h, p.q.vec);
-    } else {
-      float v[J][2][8];
-      float mx = 0.f;
+      for (int h = 0; h < 2; ++h) a[j][h] = load8_raw(p.q.p, at + 16 * g + 64 * j + 8 * h, p.q.vec);
+  }
+  __device__ __forceinline__ void take(const SplitRows<DH, 16>& rows, int n, int g) {
+    fac = rows.fac[n];
 #pragma unroll
-      for (int j = 0; j < J; ++j)
+    for (int j = 0; j < J; ++j)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          load8(p.q.p, at + 64 * j + 8 * h, p.q_lo.p ? PT_BF16 : PT_F32, p.q.vec, v[j][h]);
-          if (p.q_lo.p) {
-            float y[8];
-            load8(p.q_lo.p, at + 64 * j + 8 * h, PT_BF16, p.q.vec, y);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[j][h][i] += y[i];
-          }
-#pragma unroll
-          for (int i = 0; i < 8; ++i) mx = fmaxf(mx, fabsf(v[j][h][i]));
-        }
-      mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-      mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-      const int ex = scale_exponent(mx);
-      const float f = pow2i(8 - ex);  // the row's largest value to [2^8, 2^9)
-      fac *= pow2i(ex - 8);
-#pragma unroll
-      for (int j = 0; j < J; ++j)
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int i = 0; i < 8; i += 2) {
-            const Hilo2 x = split_f16(v[j][h][i] * f, v[j][h][i + 1] * f);
-            a[j][h][i / 2] = x.hi;
-            b[j][h][i / 2] = x.lo;
-          }
-    }
+      for (int h = 0; h < 2; ++h) {
+        a[j][h] = rows.get(0, n, 2 * (g + 4 * j) + h);
+        b[j][h] = rows.get(1, n, 2 * (g + 4 * j) + h);
+      }
   }
 
   __device__ __forceinline__ void scores(const ThinKeys<DH>& k, f32x4 (&s)[2]) const {
@@ -117,7 +92,8 @@ struct ThinQuery {
 };
 
 // Running softmax and output: lane (n, g) holds row n's reference, its own
-// slots' part of the sum, and dims 16 x + 4 g + r in o[x][r], times 2^-E.
+// slots' part of the sum, and dims 16 x + 4 g + r in o[x][r], times
+// 2^(V_LIFT - E).
 template <int DH>
 struct ThinState {
   float m, l;
@@ -146,13 +122,13 @@ __device__ __forceinline__ void attend_thin(ThinState<DH>& st, f32x4 (&s)[2], Th
     sum = ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
   };
   probs();
-  if (__any(sum > 16384.f)) {  // raise the reference to the scores' maximum
+  if (__any(sum > pow2i(P_TOP))) {  // raise the reference towards the scores' maximum
     float mx = -INFINITY;
 #pragma unroll
     for (int i = 0; i < 8; ++i) mx = fmaxf(mx, s[i / 4][i % 4]);
     mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
     mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * f;
-    const float mn = fmaxf(st.m, mx), al = __builtin_amdgcn_exp2f(st.m - mn);
+    const float mn = fmaxf(st.m, mx - P_LIFT), al = __builtin_amdgcn_exp2f(st.m - mn);
     st.m = mn;
     st.l *= al;
     st.scale(al);
@@ -163,7 +139,7 @@ __device__ __forceinline__ void attend_thin(ThinState<DH>& st, f32x4 (&s)[2], Th
     st.scale(pow2i(st.E - ve));
     st.E = ve;
   }
-  const float vs = pow2i(ve - st.E);
+  const float vs = value_factor(ve, st.E);
   if constexpr (EDGE::value) {
     // bytes that no row sees become 0, and a NaN that only some rows see is
     // given to those (as in paged_attention.hip)
@@ -218,9 +194,36 @@ __device__ __forceinline__ void attend_thin(ThinState<DH>& st, f32x4 (&s)[2], Th
   }
 }
 
-template <int QF>
-constexpr int type_of() {
-  return QF == Q_BF16 ? PT_BF16 : QF == Q_F16 ? PT_F16 : PT_F32;
+constexpr int type_of(int qf) { return qf == Q_BF16 ? PT_BF16 : qf == Q_F16 ? PT_F16 : PT_F32; }
+
+// The end of a workgroup that has all of a sequence's cached part of a KV head's
+// rows: joined by `join(row, chunk of 4 dims, m, l, o)`, the root path's nodes
+// added, and written.
+template <int DH, int QF, class Join>
+__device__ __forceinline__ void write_rows(const PagedAttn& a, const Place& p, int count, int live, Join join) {
+  constexpr int DT = type_of(QF), CH = DH / 4;
+  const int G = a.Hq / a.pool.Hkv;
+  bool bad = false;
+  checked_len(a.tab, p.b, &bad);
+  if (count < 0 || count > a.nodes) bad = true, count = min(max(count, 0), a.nodes);
+  if (bad && a.status && threadIdx.x == 0) atomicOr(a.status, PAGED_BAD_LENGTH);
+  for (int i = threadIdx.x; i < live * CH; i += blockDim.x) {  // whole rows: CH divides 64
+    const int r = i / CH, c = i % CH, node = r % a.nodes, h = p.hk * G + r / a.nodes, d = 4 * c;
+    if (node >= count) {
+      if (a.out_ks) store_row<DT>(a, p.b, node, h, d, make_float4(0.f, 0.f, 0.f, 0.f));
+      continue;
+    }
+    const uint64_t anc = anc_of(a, p.b, node);
+    const float4 q = query_quad<DT>(a, p.b * a.q.sb + node * a.q.sr + h * a.q.sh + d);
+    RootPath<DT, 4> path;
+    path.start(a, p.b, p.hk, d, anc, depth_of(anc, node), p.sight.len);
+    float m, l;
+    float4 o;
+    join(r, c, m, l, o);
+    if (m == NO_MAX && l == 0.f) m = -INFINITY;  // no slot is seen
+    path.add(a, q, CH, m, l, o);
+    store_row<DT>(a, p.b, node, h, d, row_output(l, o, bad));
+  }
 }
 
 template <int DH, int QF, int NW, bool FUSED>
@@ -232,19 +235,9 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_thin_kernel(PagedAttn a) {
   const int n = lane & 15, g = lane >> 4;
   const int G = a.Hq / a.pool.Hkv, R = G * a.nodes;
   Place p;
-  if constexpr (FUSED) {
-    p.hk = blockIdx.x % a.pool.Hkv;
-    p.b = blockIdx.x / a.pool.Hkv;
-    p.bad = false;
-    const int len = checked_len(a.tab, p.b, &p.bad);
-    p.seq = seq_tiles(len, a.cut);
-    p.i0 = 0;
-    p.i1 = p.seq.n;
-    p.sight = Sight{len, a.cut.window, a.cut.sinks};
-  } else if (!place_of(a, 1, p)) {
-    return;
-  }
-  int count = a.counts ? a.counts[p.b] : a.nodes;
+  const int blocks = FUSED ? 1 : (R + 15) / 16;
+  if (!(FUSED ? whole_sequence(a, 1, p) : place_of(a, blocks, p))) return;
+  const int count = a.counts ? a.counts[p.b] : a.nodes, first = 16 * p.rb, live = min(16, R - first);
 
   // lane j looks up the j-th of 64 of the wave's tiles i0 + w, i0 + w + NW, ..
   const int mine = p.i1 - p.i0 - w > 0 ? (p.i1 - p.i0 - w + NW - 1) / NW : 0;
@@ -259,10 +252,16 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_thin_kernel(PagedAttn a) {
     }
   };
   look(0);
-  const int row = min(n, R - 1), node = row % a.nodes, hq = p.hk * G + row / a.nodes;
+  const int node = min(first + n, R - 1) % a.nodes;
   const int pos = a.cut.window ? p.sight.len + depth_of(anc_of(a, p.b, node), node) : 0;
   ThinQuery<DH, QF> q;
-  q.load(a, p.b * a.q.sb + node * a.q.sr + hq * a.q.sh, g);
+  if constexpr (QF == Q_SPLIT) {
+    __shared__ SplitRows<DH, 16> rows;
+    rows.fill(a, [&](int r) { return query_row(a, p, first + r); });
+    q.take(rows, n, g);
+  } else {
+    q.load(a, query_row(a, p, first + n), g);
+  }
   ThinState<DH> st;
   st.m = NO_MAX;
   st.l = 0.f;
@@ -293,13 +292,14 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_thin_kernel(PagedAttn a) {
   float l = st.l + __shfl_xor(st.l, 16, 64);
   l += __shfl_xor(l, 32, 64);
   if (__any(p.bad)) l = __builtin_nanf("");  // a tile that is not there: the rows become NaN
-  if (n < R) {
-    const float fe = pow2i(st.E);
+  if (n < live) {
+    const float fe = out_factor(st.E);
 #pragma unroll
     for (int x = 0; x < DH / 16; ++x)
       so[w][n * CH + ((4 * x + g) ^ (n & 7))] =
           make_float4(st.o[x][0] * fe, st.o[x][1] * fe, st.o[x][2] * fe, st.o[x][3] * fe);
-    if (g == 0) sm[w][n] = st.m, sl[w][n] = l;
+    const float2 ml = out_sums(st.m, l);
+    if (g == 0) sm[w][n] = ml.x, sl[w][n] = ml.y;
   }
   __syncthreads();
   // the waves' results of chunk c of row r
@@ -318,10 +318,10 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_thin_kernel(PagedAttn a) {
     }
   };
   if constexpr (!FUSED) {
-    const long long prow = ((long long)p.u * a.pool.Hkv + p.hk) * R;
-    for (int i = threadIdx.x; i < R * CH; i += 64 * NW) {
+    const long long prow = ((long long)p.u * a.pool.Hkv + p.hk) * R + first;
+    for (int i = threadIdx.x; i < live * CH; i += 64 * NW) {
       const int r = i / CH, c = i % CH;
-      if (count < a.nodes && r % a.nodes >= count) continue;  // an absent node
+      if (count < a.nodes && (first + r) % a.nodes >= count) continue;  // an absent node
       float m, L;
       float4 o;
       join(r, c, m, L, o);
@@ -329,39 +329,16 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_thin_kernel(PagedAttn a) {
       if (c == 0) *reinterpret_cast<float2*>(a.part_ml + (prow + r) * 2) = make_float2(m, L);
     }
   } else {
-    constexpr int DT = type_of<QF>();
-    bool bad = false;
-    checked_len(a.tab, p.b, &bad);
-    if (count < 0 || count > a.nodes) bad = true, count = min(max(count, 0), a.nodes);
-    if (bad && a.status && threadIdx.x == 0) atomicOr(a.status, PAGED_BAD_LENGTH);
-    for (int i = threadIdx.x; i < R * CH; i += 64 * NW) {  // whole rows: CH divides 64
-      const int r = i / CH, c = i % CH, nd = r % a.nodes, h = p.hk * G + r / a.nodes, d = 4 * c;
-      if (nd >= count) {
-        if (a.out_ks) store_row<DT>(a, p.b, nd, h, d, make_float4(0.f, 0.f, 0.f, 0.f));
-        continue;
-      }
-      const uint64_t anc = anc_of(a, p.b, nd);
-      const float4 qd = query_quad<DT>(a, p.b * a.q.sb + nd * a.q.sr + h * a.q.sh + d);
-      RootPath<DT, 4> path;
-      path.start(a, p.b, p.hk, d, anc, depth_of(anc, nd), p.sight.len);
-      float m, L;
-      float4 o;
-      join(r, c, m, L, o);
-      if (m == NO_MAX && L == 0.f) m = -INFINITY;  // no slot is seen
-      path.add(a, qd, CH, m, L, o);
-      store_row<DT>(a, p.b, nd, h, d, row_output(L, o, bad));
-    }
+    write_rows<DH, QF>(a, p, count, live, join);
   }
 }
 
 template <int DH, int QF>
 void launch_form(const PagedAttn& a, hipStream_t s) {
-  if (a.fused) {
-    hipLaunchKernelGGL((paged_thin_kernel<DH, QF, 8, true>), dim3(a.batch * a.pool.Hkv), dim3(512), 0, s, a);
-  } else {
-    const int wgs = (a.units * a.pool.Hkv + 7) / 8 * 8;
-    hipLaunchKernelGGL((paged_thin_kernel<DH, QF, 4, false>), dim3(wgs), dim3(256), 0, s, a);
-  }
+  const int parts = a.fused ? a.batch : a.units;  // whole sequences, or units
+  const int R = a.Hq / a.pool.Hkv * a.nodes, wgs = (parts * a.pool.Hkv + 7) / 8 * 8 * ((R + 15) / 16);
+  if (a.fused) hipLaunchKernelGGL((paged_thin_kernel<DH, QF, 8, true>), dim3(wgs), dim3(512), 0, s, a);
+  else hipLaunchKernelGGL((paged_thin_kernel<DH, QF, 4, false>), dim3(wgs), dim3(256), 0, s, a);
 }
 
 }  // namespace

@@ -27,6 +27,11 @@ pytestmark = pytest.mark.gpu
 DT = {"bf16": torch.bfloat16, "f16": torch.float16, "f32": torch.float32}
 
 
+@pytest.fixture(autouse=True)
+def same_numbers():
+    torch.manual_seed(0)
+
+
 @pytest.fixture(scope="module")
 def G():
     import paper_2502_11018_amd as pkg
@@ -441,6 +446,59 @@ def test_large_and_small_scores(G):
             q, k5, v5 = (t[0].double().cpu().numpy() for t in x)
             o, mag, top = OP.attention(q, k5, v5, ck, cv, OP.visible(512, chain(5)))
             check(out[0].double().cpu().numpy(), o, mag, top, 64, 517, dtype)
+
+
+FORMS = [(5, 1, 1, 300), (12, 4, 1, 900), (24, 2, 1, 900), (64, 2, 1, 7000), (64, 4, 4, 16400)]  # nodes, group, batch, slots
+
+
+def winner(G, nodes, group, batch, length, dtype, q0, k, v):
+    """Slot 0's score far above the others': scores q0 k / 8, exact."""
+    heads = 4
+    pool, _ = make_pool(G, batch * -(-length // 64), heads, 64, 64)
+    table = tables(batch, -(-length // 64), batch * -(-length // 64))
+    zero = torch.zeros(batch, dtype=torch.int32, device="cuda")
+    keys = torch.zeros(batch, length, heads, 64, device="cuda")
+    keys[..., 0] = -k
+    keys[:, 0, :, 0] = k
+    G.paged_append(pool, table, zero, keys, v.view(1, -1, 1, 64).expand(batch, length, heads, 64).contiguous())
+    q = torch.zeros(batch, nodes, heads * group, 64, device="cuda")
+    own = torch.zeros(batch, nodes, heads, 64, device="cuda")
+    q[..., 0] = q0
+    own[..., 0] = -8 * k
+    out = G.paged_attention(pool, table, zero + length, q.to(DT[dtype]), own.to(DT[dtype]), torch.zeros_like(own).to(DT[dtype]))
+    return out.double().cpu()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("nodes,group,batch,length", FORMS)
+def test_many_small_probabilities(G, nodes, group, batch, length, dtype):
+    """Weights of 2^-26 beside one of 1 still count: they stand at 2^-18 or
+    above in fp16, whose steps of 2^-24 round them by 2^-7, their scores' terms
+    by far less."""
+    v = torch.full((length, 64), 64.0, device="cuda")
+    v[0] = 0
+    out = winner(G, nodes, group, batch, length, dtype, 9.0, 8.0, v)
+    part = (length - 1) * np.exp(-18.0)
+    tol = 2.0**-7 + 2.0**-12 + torch.finfo(DT[dtype]).eps / 2 + (2.0**-25 / (64 * part) if dtype == "f16" else 0)
+    assert (out / (64 * part / (1 + part)) - 1).abs().max().item() <= tol
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("nodes,group,batch,length", FORMS)
+@pytest.mark.parametrize("spread", [20, 21])
+def test_small_values_beside_large_ones(G, nodes, group, batch, length, dtype, spread):
+    """The row of a slot whose tile's values are 2^-20 of other tiles' is that
+    slot's: its bytes times powers of two, its weight over a sum of weights
+    whose exponents near 29 are rounded by 2^-20."""
+    v = torch.full((length, 64), 1.75, device="cuda")
+    v[:32] = 1.75 * 2.0**-20
+    i = torch.arange(64, device="cuda")  # four bits each, down to e4m3's last: exact at the tile's exponent of -28
+    v[0] = (i % 16) * 2.0**-26 * torch.tensor([1, 2.0**-4, 2.0**-8, 2.0**-11], device="cuda")[i // 16]
+    v[32 * (length // 64):] *= 2.0**(spread - 20)
+    out = winner(G, nodes, group, batch, length, dtype, 20.0, 8.0, v)
+    want = v[0].double().cpu()
+    # the others' weights: exp(-40) each, values up to 3.5
+    assert ((out - want).abs() <= want * (2.0**-19 + torch.finfo(DT[dtype]).eps / 2) + 3.5 * length * np.exp(-40.0)).all()
 
 
 def test_nan_in_masked_places(G):
