@@ -509,8 +509,10 @@ typedef struct griffin_attention {
  * place holds, NaN included, reaches no row.
  *   max_length: no length is larger (it bounds the launch); -1: the table's
  *               capacity.
- * Scores, probabilities' sums and outputs are fp32; fp32 inputs enter the
- * matrix cores as two fp16 parts, others' probabilities as one.  The rows of a
+ * Scores, probabilities' sums and outputs are fp32.  fp32 inputs enter the
+ * matrix cores as two fp16 parts (22 bits), their and fp16 inputs'
+ * probabilities too, bf16 inputs' as one (11 bits); a probability is rounded by
+ * 2^-33 of the row's largest at least.  The rows of a
  * sequence with an invalid page or length become NaN.  Head h reads KV head
  * h / (n_q_heads / n_kv_heads).  The workspace (16-byte aligned, of
  * griffin_paged_attention_workspace bytes; 0 for arguments that the call
@@ -528,8 +530,8 @@ int griffin_paged_attention(const griffin_attention *args, void *workspace, size
  * The context works as one of griffin_verify_init (steps, both acceptances,
  * features, graphs), with these differences: a step writes nothing to the
  * cache (the nodes' K/V stay with the context in fp32), and griffin_commit
- * appends the root and the accepted nodes, rounded once.  A draft context may
- * not be built on it.  Errors: as griffin_verify_init. */
+ * appends the root and the accepted nodes, rounded once.  Errors: as
+ * griffin_verify_init. */
 int griffin_verify_init_paged(const griffin_model_desc *desc, const griffin_weights *weights, const griffin_pool *pool,
                               int32_t window, int32_t sinks, void *hip_stream, griffin_ctx **out);
 

@@ -71,6 +71,10 @@ hipError_t launch_paged_append(PagedAppend a, hipStream_t s);
 // Work cut of an attention call.  The cached tiles that any node of sequence b
 // sees (seq_tiles) are dealt to units_of(n_b) units; units are numbered
 // sequence after sequence.
+// Workgroups of a launch at most: 2^32 threads of 512 each, and room for rounding
+// up.
+constexpr long long PAGED_MAX_GROUPS = 1 << 22;
+
 struct PagedCut {
   int window, sinks;
   int target;  // units wanted in all: workgroups that fit the chip at once

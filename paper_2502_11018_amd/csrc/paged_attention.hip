@@ -795,7 +795,7 @@ int paged_plan(PagedAttn& a, int max_length) {
   // against 7 + 5), else up to 160 (16 chains over up to 2048 slots 14 us against
   // 13 + 5, 16 tokens with a window of 4096 28 against 26 + 5).
   const long long wgs = (long long)a.batch * a.pool.Hkv;
-  a.fused = R <= 16 && wgs < (1 << 30) && most <= (wgs < 128 ? 72 : 160);
+  a.fused = R <= 16 && most <= (wgs < 128 ? 72 : 160);
   const int streams = a.pool.Hkv * (a.wide ? wide_blocks : a.thin ? thin_blocks : (R + 31) / 32);
   // workgroups that fit the 256 CUs at once
   a.cut.target = std::max(1, (a.thin ? 1024 : a.wide == 8 ? 256 : 512) / streams);
@@ -803,7 +803,7 @@ int paged_plan(PagedAttn& a, int max_length) {
   a.cut.full = a.wide ? 0 : a.thin ? 64 : 32;
   // units of a sequence of n tiles: ceil(n / per) with per >= least and >= all tiles / target
   a.units = a.fused ? 0 : (int)std::min<long long>(by_len, (long long)a.cut.target + a.batch);
-  return 0;
+  return (a.units + 8LL) * streams <= PAGED_MAX_GROUPS ? 0 : -1;
 }
 
 size_t paged_workspace(PagedAttn& a, void* base) {
@@ -843,7 +843,6 @@ hipError_t launch_paged_attention(const PagedAttn& a, hipStream_t s) {
     if (e != hipSuccess || a.fused) return e;
   } else if (a.units > 0) {
     const long long wgs = ((long long)a.units * a.pool.Hkv + 7) / 8 * 8 * ((R + rows - 1) / rows);
-    if (wgs > 0x7fffffffLL) return hipErrorInvalidValue;
     if (a.pool.dh == 128) launch_form<128>(a, dim3((unsigned)wgs), s);
     else launch_form<64>(a, dim3((unsigned)wgs), s);
   }

@@ -48,6 +48,11 @@ int paged_pool_of(const griffin_pool& p, PagedPool* out) {
   return GRIFFIN_OK;
 }
 
+bool paged_sizes(const PagedPool& pool, int batch, int nodes, int n_q_heads) {
+  return (long long)batch * nodes <= PAGED_MAX_GROUPS && (long long)batch * pool.Hkv <= PAGED_MAX_GROUPS &&
+         (long long)n_q_heads * nodes <= (1 << 18);
+}
+
 // max_length < 0: the table's capacity
 int paged_table_of(const griffin_pool& pool, const int32_t* table, int stride, int cols, const int32_t* lengths,
                    int max_length, PagedTable* out) {
@@ -76,8 +81,7 @@ int attention_args(const griffin_attention* g, PagedAttn* out) {
   if (g->batch < 1 || g->window < 0 || g->sinks < 0 || !(g->scale > 0.f) || !std::isfinite(g->scale)) return GRIFFIN_EINVAL;
   if (g->nodes < 1 || g->nodes > 64) return GRIFFIN_ETREE;
   if (g->n_q_heads < 1 || g->n_q_heads % a.pool.Hkv != 0) return GRIFFIN_ESHAPE;
-  // rows and workgroups are counted in 32 bits
-  if ((long long)g->batch * g->nodes > (1 << 24) || (long long)g->n_q_heads * g->nodes > (1 << 20)) return GRIFFIN_ESHAPE;
+  if (!paged_sizes(a.pool, g->batch, g->nodes, g->n_q_heads)) return GRIFFIN_ESHAPE;
   a.dtype = g->dtype;
   a.batch = g->batch;
   a.nodes = g->nodes;
@@ -106,7 +110,7 @@ int griffin_paged_append(const griffin_append* g, void* hip_stream) {
   rc = paged_table_of(g->pool, g->table, g->table_stride, g->table_cols, g->lengths, -1, &a.tab);
   if (rc != GRIFFIN_OK) return rc;
   if (g->max_new == 0) return GRIFFIN_OK;
-  if ((long long)g->batch * (g->max_new / 32 + 2) * a.pool.Hkv > 0x7fffffffLL) return GRIFFIN_ESHAPE;
+  if ((long long)g->batch * (g->max_new / 32 + 2) > PAGED_MAX_GROUPS) return GRIFFIN_ESHAPE;
   a.counts = g->counts;
   a.counts_stride = 1;
   a.path = g->path;

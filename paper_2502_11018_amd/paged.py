@@ -54,6 +54,10 @@ def paged_read(pool: Sequence[torch.Tensor], table: torch.Tensor, n: int):
     (k, v), each [Hkv, n, dh]."""
     k, v, ke, ve = pool
     pages = table[: -(-n // (k.shape[2] * 32))].long()
+    if n < 0 or table.dim() != 1 or len(pages) * k.shape[2] * 32 < n:
+        raise ValueError(f"the table does not hold {n} slots")
+    if len(pages) and not 0 <= int(pages.min()) <= int(pages.max()) < k.shape[0]:
+        raise ValueError("a page is not in the pool")
     fk = torch.ldexp(k[pages].float(), ke[pages].int()[..., None, None, None])  # [p, Hkv, t, dh/16, 32, 16]
     fv = torch.ldexp(v[pages].float(), ve[pages].int()[..., None, None])        # [p, Hkv, t, dh, 32]
     fk = fk.permute(1, 0, 2, 4, 3, 5).reshape(k.shape[1], -1, v.shape[3])
@@ -105,10 +109,22 @@ def _rows(t: torch.Tensor, what: str, dev, dtype, shape):
     return t.data_ptr(), s[0], s[1], s[2]
 
 
-def _on(dev, stream):
-    """The context that makes `stream`, ordered after the caller's, current."""
-    stream.wait_stream(torch.cuda.current_stream(dev))
-    return torch.cuda.stream(stream)
+def _on(stream, call, pool, *tensors, **named):
+    """call(pool, *tensors, **named) with `stream`, ordered after the caller's,
+    current.  The allocator learns of it: no tensor's memory is used again
+    before the stream's work with it has ended."""
+    if stream.device != pool[0].device:
+        raise ValueError("the stream must be one of the pool's device")
+    here = torch.cuda.current_stream(stream.device)
+    stream.wait_stream(here)
+    with torch.cuda.stream(stream):
+        out = call(pool, *tensors, **named)
+    for t in (*pool, *tensors, *named.values()):
+        if isinstance(t, torch.Tensor):
+            t.record_stream(stream)
+    if out is not None and named.get("out") is None:
+        out.record_stream(here)
+    return out
 
 
 def _call(fn, dev, *args):
@@ -136,8 +152,8 @@ def paged_append(pool: Sequence[torch.Tensor], table: torch.Tensor, lengths: tor
     rotated already); status: an int32 tensor of one element that collects
     GRIFFIN_PAGED_* bits of what the device found out of range."""
     if stream is not None:
-        with _on(k.device, stream):
-            return paged_append(pool, table, lengths, k, v, counts=counts, path=path, rope_base=rope_base, status=status)
+        return _on(stream, paged_append, pool, table, lengths, k, v, counts=counts, path=path, rope_base=rope_base,
+                   status=status)
     fields, heads, dh, dev = _pool_fields(pool)
     b, cols, stride, lens = _table(table, lengths, dev)
     dtype = k.dtype
@@ -179,9 +195,8 @@ def paged_attention(pool: Sequence[torch.Tensor], table: torch.Tensor, lengths: 
     out: rows of absent nodes are left as they were (None: new, they are zero);
     status: as for paged_append."""
     if stream is not None:
-        with _on(q.device, stream):
-            return paged_attention(pool, table, lengths, q, k, v, anc=anc, counts=counts, window=window, sinks=sinks,
-                                   scale=scale, max_length=max_length, out=out, status=status)
+        return _on(stream, paged_attention, pool, table, lengths, q, k, v, anc=anc, counts=counts, window=window,
+                   sinks=sinks, scale=scale, max_length=max_length, out=out, status=status)
     fields, heads, dh, dev = _pool_fields(pool)
     b, cols, stride, lens = _table(table, lengths, dev)
     dtype = q.dtype

@@ -232,7 +232,7 @@ class TreeVerifier:
         in the sequence's pages, rounded to 8 bits (fp16 and fp32 too)."""
         if self.pool is not None:
             n = -(-k.shape[1] // self._pool_desc.page_slots)
-            if (self.pages[seq, :n] < 0).any():
+            if k.shape[1] > self.kv_capacity or (self.pages[seq, :n] < 0).any():
                 raise ValueError("write_prefix: a page of the prefix is not set")
             table = torch.from_numpy(self.pages[seq:seq + 1, :n].copy()).to(self.device)
             paged_append(layer_pool(self.pool, layer), table, torch.zeros(1, dtype=torch.int32, device=self.device),

@@ -118,6 +118,8 @@ def attention_args(**kw):
     ("ETREE", dict(nodes=0)), ("ETREE", dict(nodes=65)), ("ESHAPE", dict(hq=3)), ("ESHAPE", dict(hq=0)), ("ESHAPE", dict(dh=32)),
     ("ESHAPE", dict(n=0)), ("ESHAPE", dict(page=33)), ("ECAPACITY", dict(most=129)), ("ESHAPE", dict(b=1 << 24)),
     ("ESHAPE", dict(hq=1 << 20)), ("ESHAPE", dict(cols=1 << 26, stride=1 << 26)),
+    ("ESHAPE", dict(b=1 << 22)), ("ESHAPE", dict(hq=1 << 18)), ("ESHAPE", dict(b=1 << 20, heads=8, hq=8)),
+    ("ESHAPE", dict(b=1 << 15, nodes=64, hq=4096, heads=1, most=32)),
 ])
 def test_attention_refuses(code, kw):
     N = _lib()
@@ -195,3 +197,15 @@ def test_binding_checks_tensors():
 def test_struct_layouts():
     """The packed arguments have the sizes of the C structs (192 and 256 bytes)."""
     assert len(append_args()) == 192 and len(attention_args()) == 256 and struct.calcsize("@P") == 8
+
+
+def test_read_refuses_what_the_table_does_not_hold():
+    import torch
+    from paper_2502_11018_amd import paged_pool, paged_read
+    pool = paged_pool(2, 1, 64, 32, device="cpu")
+    for pages, n in ([0, 1], 65), ([0, 2], 64), ([-1], 1), ([0], -1):
+        with pytest.raises(ValueError):
+            paged_read(pool, torch.tensor(pages, dtype=torch.int32), n)
+    k, v = paged_read(pool, torch.tensor([1, 5], dtype=torch.int32), 32)  # the second page is not read
+    assert k.shape == v.shape == (1, 32, 64)
+    assert paged_read(pool, torch.tensor([], dtype=torch.int32), 0)[0].shape == (1, 0, 64)

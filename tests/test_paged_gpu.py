@@ -660,6 +660,35 @@ def test_prompt_and_decoding_together(G, dtype, window):
     same_cache(pool, cache)
 
 
+def test_temporaries_on_another_stream(G):
+    """What only a call on another stream still needs is not given to the next
+    tensor of the caller's."""
+    pool, cache = make_pool(G, 8, 2, 64, 128)
+    table = tables(2, 4, 8)
+    fill(G, pool, cache, table, [30, 100], 0)
+    n = torch.tensor([30, 100], dtype=torch.int32, device="cuda")
+    x = torch.randn(2, 16, 8, 128, device="cuda").to(torch.bfloat16)
+    q, k, v = (t.contiguous() for t in x.split([4, 2, 2], 2))
+    want = G.paged_attention(pool, table, n, q, k, v)
+    raw = [t.view(torch.uint8) for t in pool]
+    before = [t.clone() for t in raw]
+    G.paged_append(pool, table, n, k, v)
+    full = [t.clone() for t in raw]
+    for s, t in zip(raw, before):
+        s.copy_(t)
+    side, busy = torch.cuda.Stream(), torch.randn(4096, 4096, device="cuda")
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        for _ in range(20):
+            busy = busy @ busy * 1e-3
+    out = G.paged_attention(pool, table.clone(), n.clone(), q.clone(), k.clone(), v.clone(), stream=side)
+    G.paged_append(pool, table.clone(), n.clone(), k.clone(), v.clone(), stream=side)
+    over = [torch.zeros_like(t) for t in (table, n, q, k, v, out) for _ in range(3)]
+    torch.cuda.synchronize()
+    assert torch.equal(out, want) and not any(t.any() for t in over)
+    assert all(torch.equal(s, t) for s, t in zip(raw, full))
+
+
 def test_other_stream_and_captured(G):
     """The calls on a stream of their own, and captured: replays follow the
     lengths and rows that changed in place, with eager work between them."""

@@ -314,6 +314,9 @@ def test_refusals():
         p.v.commit()
         mw = p.mw.to("cuda")
         args = dict(max_batch=1, max_tree=16, max_depth=15, kv_capacity=128)
+        rows = torch.zeros(p.m.n_kv_heads, cap + 1, p.m.head_dim, dtype=torch.bfloat16, device="cuda")
+        with pytest.raises(ValueError):
+            p.v.write_prefix(0, 0, rows, rows)
         with pytest.raises(ValueError):
             G.TreeVerifier(p.m, mw, window=64, **args)
         with pytest.raises(ValueError):
