@@ -164,6 +164,7 @@ struct griffin_ctx {
   long long pool_layer = 0;     // tiles of one layer
   int window = 0, sinks = 0, cols = 0;
   int length_bound = 0;         // of this step's prefix lengths, a power of two or the capacity
+  int node_bound = 0;           // of its trees' nodes, a power of four or max_tree
   std::vector<int32_t> table;   // [max_batch][cols] pages, -1: none
   int32_t* table_dev = nullptr;
   int32_t* table_host = nullptr;  // pinned staging
@@ -199,7 +200,7 @@ struct griffin_ctx {
     int batch;
     float* logits;
     bool kv_only;
-    int tree_k, tree_depth, tree_n;  // 0: one pass
+    int tree_k, tree_depth, tree_n;  // 0: one pass (paged: tree_n minus its bound of nodes)
     int slots;                       // partial slots the merge reads (paged: the bound of the prefix lengths)
     int half;                        // griffin_ctx::half (a draft tree's passes set their own)
     hipGraphExec_t exec;
@@ -361,6 +362,13 @@ int length_bound(int longest, int capacity) {
   return (int)std::min<long long>(b, capacity);
 }
 
+// The bound of a step's nodes: a single token and short chains run as such.
+int node_bound(int most, int max_tree) {
+  int n = 1;
+  while (n < most) n *= 4;
+  return std::min(n, max_tree);
+}
+
 // Whether every page that a step of sequence b reads, or that committing up to
 // `more` tokens behind its prefix writes, is set.
 bool has_pages(const griffin_ctx* c, int b, int prefix, int more) {
@@ -376,15 +384,16 @@ bool has_pages(const griffin_ctx* c, int b, int prefix, int more) {
 }
 
 // A paged context's attention over `batch` sequences whose prefixes are at most
-// `bound` slots, without its buffers.
-int paged_shape(const griffin_ctx* c, int batch, int bound, PagedAttn* a) {
+// `bound` slots and whose trees have at most `nodes` nodes, without its buffers.
+int paged_shape(const griffin_ctx* c, int batch, int bound, int nodes, PagedAttn* a) {
   const griffin_model_desc& d = c->d;
   *a = PagedAttn{};
   a->pool = c->pool;
   a->tab = PagedTable{c->table_dev, c->cols, c->cols, c->meta.prefix_len, bound};
   a->dtype = PT_F32;
   a->batch = batch;
-  a->nodes = d.max_tree;
+  a->nodes = nodes;
+  a->stride = d.max_tree;
   a->Hq = d.n_q_heads;
   a->cut.window = c->window;
   a->cut.sinks = c->window ? c->sinks : 0;
@@ -405,7 +414,7 @@ PagedRows tree_rows(const griffin_model_desc& d, const float* p) {
 hipError_t paged_attention_of(griffin_ctx* c, int layer, float scale_log2, hipStream_t s) {
   const griffin_model_desc& d = c->d;
   PagedAttn a;
-  if (paged_shape(c, c->batch, c->length_bound, &a) != 0) return hipErrorInvalidValue;
+  if (paged_shape(c, c->batch, c->length_bound, c->node_bound, &a) != 0) return hipErrorInvalidValue;
   const long long tiles = layer * c->pool_layer, bytes = tiles * 32 * d.head_dim;
   a.pool.k += bytes;
   a.pool.v += bytes;
@@ -655,7 +664,9 @@ int run_graph(griffin_ctx* c, const griffin_ctx::GraphEntry& key, Body body) {
 
 // One pass (batch, logits_out, kv_only from the context).
 int run_pass(griffin_ctx* c, float* logits_out) {
-  return run_graph(c, {c->batch, logits_out, c->kv_only, 0, 0, 0, c->paged ? c->length_bound : c->comb_slots, c->half, nullptr},
+  // (paged: the nodes' bound in tree_n's place, negative; a draft tree's is positive)
+  return run_graph(c, {c->batch, logits_out, c->kv_only, 0, 0, c->paged ? -c->node_bound : 0,
+                       c->paged ? c->length_bound : c->comb_slots, c->half, nullptr},
                    [&]() { return enqueue_pass(c, logits_out); });
 }
 
@@ -934,12 +945,15 @@ static int verify_init(const griffin_model_desc* desc, const griffin_weights* w,
     size_t most = 0;  // of every batch and bound that a step can have
     for (int b = 1; b <= d.max_batch; ++b)
       for (int bound = length_bound(0, d.kv_capacity);; bound = length_bound(bound + 1, d.kv_capacity)) {
-        PagedAttn a;
-        if (paged_shape(c, b, bound, &a) != 0) {
-          griffin_verify_free(c);
-          return GRIFFIN_ESHAPE;
+        for (int nodes = 1;; nodes = node_bound(nodes + 1, d.max_tree)) {
+          PagedAttn a;
+          if (paged_shape(c, b, bound, nodes, &a) != 0) {
+            griffin_verify_free(c);
+            return GRIFFIN_ESHAPE;
+          }
+          most = std::max(most, paged_workspace(a, nullptr));
+          if (nodes == d.max_tree) break;
         }
-        most = std::max(most, paged_workspace(a, nullptr));
         if (bound == d.kv_capacity) break;
       }
     ALLOC(c->paged_ws, most);
@@ -1145,7 +1159,10 @@ int griffin_verify_step(griffin_ctx* c, int32_t batch, const int32_t* prefix_len
     if (c->paged && !has_pages(c, b, prefix_len[b], *std::max_element(depth, depth + n_nodes[b]) + 1))
       return set_err(c, GRIFFIN_ECAPACITY, "sequence " + std::to_string(b) + ": a page of the step is not set");
   }
-  if (c->paged) c->length_bound = length_bound(*std::max_element(prefix_len, prefix_len + batch), d.kv_capacity);
+  if (c->paged) {
+    c->length_bound = length_bound(*std::max_element(prefix_len, prefix_len + batch), d.kv_capacity);
+    c->node_bound = node_bound(*std::max_element(n_nodes, n_nodes + batch), d.max_tree);
+  }
   // fill the staging buffer not used by the previous step's copy
   const int k = c->meta_cur ^ 1;
   HIP_TRY(c, hipEventSynchronize(c->meta_ev[k]));

@@ -93,6 +93,7 @@ struct PagedAttn {
   int out_vec;
   int out_ks;             // > 0: out is the split bf16 packed operand of a projection (xpack_off), out_ks K steps
   int dtype, batch, nodes, Hq;
+  int stride;             // nodes of a sequence in anc and in the packed operand, >= nodes
   float scale_log2;       // log2(e) * scale
   PagedCut cut;
   int units;              // upper bound of the units (grid)

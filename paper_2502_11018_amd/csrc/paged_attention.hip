@@ -684,11 +684,15 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(PagedAttn a) {
   __shared__ float4 so[SG > 1 ? 256 : 1];
   __shared__ float2 sml[SG > 1 ? 256 : 1];
   const int dh = a.pool.dh, quads = dh / 4, heads = 256 / SG / quads;  // heads of a workgroup
-  const int b = blockIdx.x / a.nodes, i = blockIdx.x % a.nodes;
+  const int b = blockIdx.x / a.stride, i = blockIdx.x % a.stride;
   const int G = a.Hq / a.pool.Hkv, R = G * a.nodes;
   const int grp = SG == 1 ? 0 : threadIdx.x / (256 / SG), t = SG == 1 ? threadIdx.x : threadIdx.x % (256 / SG);
   const int h = min((int)blockIdx.y * heads + t / quads, a.Hq - 1), d = t % quads * 4, hk = h / G;
   const bool mine = blockIdx.y * heads + t / quads < a.Hq;
+  if (i >= a.nodes) {  // uniform: a row of the operand behind the nodes
+    if (a.out_ks && grp == 0 && mine) store_row<DT>(a, b, i, h, d, make_float4(0.f, 0.f, 0.f, 0.f));
+    return;
+  }
   const uint64_t anc = anc_of(a, b, i);
   const int2 un = a.units > 0 ? a.first_unit[b] : make_int2(0, 0);
   bool bad = false;
@@ -830,7 +834,7 @@ static void launch_form(const PagedAttn& a, dim3 grid, hipStream_t s) {
 
 template <int DT>
 static void launch_combine(const PagedAttn& a, bool few, hipStream_t s) {
-  const int rows = a.batch * a.nodes, threads = a.Hq * (a.pool.dh / 4);
+  const int rows = a.batch * a.stride, threads = a.Hq * (a.pool.dh / 4);
   if (few) hipLaunchKernelGGL((paged_combine_kernel<DT, 4>), dim3(rows, (threads + 63) / 64), dim3(256), 0, s, a);
   else hipLaunchKernelGGL((paged_combine_kernel<DT, 1>), dim3(rows, (threads + 255) / 256), dim3(256), 0, s, a);
 }

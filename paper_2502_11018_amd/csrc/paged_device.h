@@ -104,7 +104,7 @@ __device__ __forceinline__ bf16x8 cvt8_bf16(uint32_t a, uint32_t b) {
 
 // nodes that node i sees, and its position behind the cached slots
 __device__ __forceinline__ uint64_t anc_of(const PagedAttn& a, int b, int i) {
-  return a.anc ? a.anc[(long long)b * a.nodes + i] & (~0ull >> (64 - a.nodes)) : (2ull << i) - 1;
+  return a.anc ? a.anc[(long long)b * a.stride + i] & (~0ull >> (64 - a.nodes)) : (2ull << i) - 1;
 }
 __device__ __forceinline__ int depth_of(uint64_t anc, int i) { return __builtin_popcountll(anc & ~(1ull << i)); }
 
@@ -417,7 +417,7 @@ __device__ __forceinline__ float4 row_output(float l, const float4& o, bool bad)
 template <int DT>
 __device__ __forceinline__ void store_row(const PagedAttn& a, int b, int i, int h, int d, const float4& out) {
   if (a.out_ks) {
-    uint16_t* dst = static_cast<uint16_t*>(a.out) + xpack_off((long long)b * a.nodes + i, h * a.pool.dh + d, a.out_ks);
+    uint16_t* dst = static_cast<uint16_t*>(a.out) + xpack_off((long long)b * a.stride + i, h * a.pool.dh + d, a.out_ks);
     const Hilo2 p0 = pack_hilo2(out.x, out.y), p1 = pack_hilo2(out.z, out.w);
     *reinterpret_cast<uint2*>(dst) = make_uint2(p0.hi, p1.hi);
     *reinterpret_cast<uint2*>(dst + XPACK_LO) = make_uint2(p0.lo, p1.lo);

@@ -84,7 +84,7 @@ int attention_args(const griffin_attention* g, PagedAttn* out) {
   if (!paged_sizes(a.pool, g->batch, g->nodes, g->n_q_heads)) return GRIFFIN_ESHAPE;
   a.dtype = g->dtype;
   a.batch = g->batch;
-  a.nodes = g->nodes;
+  a.nodes = a.stride = g->nodes;
   a.Hq = g->n_q_heads;
   a.scale_log2 = (float)((double)g->scale * 1.4426950408889634);
   a.cut.window = g->window;

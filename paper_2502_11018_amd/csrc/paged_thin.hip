@@ -224,6 +224,9 @@ __device__ __forceinline__ void write_rows(const PagedAttn& a, const Place& p, i
     path.add(a, q, CH, m, l, o);
     store_row<DT>(a, p.b, node, h, d, row_output(l, o, bad));
   }
+  if (a.out_ks)  // the operand's rows behind them
+    for (int i = threadIdx.x; i < (a.stride - a.nodes) * G * CH; i += blockDim.x)
+      store_row<DT>(a, p.b, a.nodes + i / (G * CH), p.hk * G + i / CH % G, i % CH * 4, make_float4(0.f, 0.f, 0.f, 0.f));
 }
 
 template <int DH, int QF, int NW, bool FUSED>

@@ -107,6 +107,29 @@ def test_step_matches_oracle(name):
         p.v.close()
 
 
+@pytest.mark.parametrize("name,window", [("small-gqa", 0), ("small-gqa", 40), ("small-mha", 0)])
+def test_steps_of_few_and_many_nodes(name, window):
+    """One context's steps of 1 to max_tree nodes, mixed in a batch, on both
+    sides of the launches' bounds, each against the oracle."""
+    p = Paged(name, window, 4 if window else 0, max_tree=23)
+    try:
+        sizes = [(1,), (2,), (4,), (5,), (16,), (17,), (23,), (1, 3), (2, 20), (1,), (7, 1)]
+        for k, ns in enumerate(sizes):
+            trees = []
+            for b in range(p.B):
+                rng = np.random.default_rng(10 * k + b)
+                n = ns[b % len(ns)]
+                parents = sorted([int(rng.integers(max(0, i - 4), i)) for i in range(1, n)])
+                t = gen.chain_tree(int(rng.integers(p.m.vocab)), rng.integers(0, p.m.vocab, n - 1).tolist())
+                trees.append(type(t)(t.tokens, np.array([-1] + parents, dtype=t.parents.dtype)))
+            lg, pred, acc = p.step(trees)
+            for b, tree in enumerate(trees):
+                H.check_parity(seq(tree, p.reference(b, tree)), lg[b, : tree.n], pred[b, : tree.n], acc.sequence(b))
+                assert np.isnan(lg[b, tree.n:]).all()
+    finally:
+        p.v.close()
+
+
 @pytest.mark.parametrize("window,sinks", [(40, 0), (70, 4), (33, 40), (4096, 4)])
 def test_windowed_step_matches_oracle(window, sinks):
     """Pages that no node of the step sees are not set, and hold NaN."""
