@@ -680,7 +680,7 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_wide_kernel(PagedAttn a) {
 template <int DT, int SG>
 __global__ __launch_bounds__(256) void paged_combine_kernel(PagedAttn a) {
   constexpr int TB = SG == 1 ? 2 : 8;                  // units at a time
-  constexpr int TN = SG == 1 && DT == PT_F32 ? 4 : 8;  // nodes at a time
+  constexpr int TN = SG == 1 ? 4 : 8;  // nodes at a time
   __shared__ float4 so[SG > 1 ? 256 : 1];
   __shared__ float2 sml[SG > 1 ? 256 : 1];
   const int dh = a.pool.dh, quads = dh / 4, heads = 256 / SG / quads;  // heads of a workgroup
