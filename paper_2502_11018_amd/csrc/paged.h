@@ -68,13 +68,13 @@ struct PagedAppend {
 };
 hipError_t launch_paged_append(PagedAppend a, hipStream_t s);
 
-// Work cut of an attention call.  The cached tiles that any node of sequence b
-// sees (seq_tiles) are dealt to units_of(n_b) units; units are numbered
-// sequence after sequence.
 // Workgroups of a launch at most: 2^32 threads of 512 each, and room for rounding
 // up.
 constexpr long long PAGED_MAX_GROUPS = 1 << 22;
 
+// Work cut of an attention call.  The cached tiles that some node of a sequence
+// sees are dealt to units, numbered sequence by sequence (unit_at); each unit is
+// one partial result per row, joined by paged_combine_kernel.
 struct PagedCut {
   int window, sinks;
   int target;  // units wanted in all: workgroups that fit the chip at once
@@ -100,7 +100,7 @@ struct PagedAttn {
   float* part_o;          // [units][Hkv][G * nodes][dh]
   float* part_ml;         // [units][Hkv][G * nodes][2]
   int2* first_unit;       // [batch] first unit and units of a sequence that has any
-  // the kernel (paged_plan): at most 16 rows a KV head: thin, fused where it needs no joining; else
+  // the kernel (paged_plan).  thin: row tiles of 16, fused: whole sequences, nothing to join; else
   // wide: waves of a workgroup of the wide kernel, or 0
   int thin, fused, wide;
   int32_t* status;

@@ -5,23 +5,26 @@
 // window == 0, p - s < window or s < sinks, and the nodes of anc[i], the r-th
 // of which stands at position length + r, by the same window.
 //
-// paged_attention_kernel computes the cached part in units: some of the tiles
-// of one sequence, a KV head, and 32 rows of the head group (row = head * N +
-// node).  Its four waves take every fourth tile each and meet in LDS at the
-// end.  Per tile a wave loads 16 bytes a lane and piece, which are the matrix
-// operands as they stand, and computes S^T = K Q^T and O^T += V^T P^T with
-// v_mfma_f32_32x32x16_f16, so that a lane owns a query row and the softmax is
+// The cached part is computed in units: some of the tiles of one sequence, a KV
+// head, and a block of the head group's rows (row = head * N + node), as many
+// units as fill the chip (paged_plan, unit_at).  Three kernels for it: row tiles
+// of 32 here, of 16 for few rows and short calls (paged_thin.hip), and
+// paged_wide_kernel for many rows over long sequences.
+//
+// Per tile a wave loads 16 bytes a lane and piece, which are the matrix operands
+// as they stand, and computes S^T = K Q^T and O^T += V^T P^T with
+// v_mfma_f32_32x32x16, so that a lane owns a query row and the softmax is
 // lane-local:
-//  * e4m3 is exact in fp16.  Keys are converted as they are, their tile's
-//    exponent goes into the score's factor; values are converted relative to
-//    the largest exponent the wave has met (E), which is uniform over the wave
+//  * e4m3 is exact in fp16 and bf16.  Keys are converted as they are, their
+//    tile's exponent goes into the score's factor; values are converted relative
+//    to the largest exponent the wave has met (E), which is uniform over the wave
 //    and rarely rises; the accumulators follow it when it does.
 //  * Keys meet the matrix cores in a permuted row order, so that accumulator
 //    register r of lane half h holds slot 16 h + r: the P operand is the lane's
 //    own registers and the V operand 16 consecutive slots of a dim.
-//  * q is scaled by a power of two per row to fill fp16 (exact for bf16 and
-//    fp16 inputs); fp32 inputs enter as high and low parts (22 bits), and so
-//    do their probabilities.  The others' probabilities are rounded to fp16,
+//  * bf16 and fp16 queries are operands as they are; fp32 ones, scaled by a power
+//    of two per row to fill fp16, enter as high and low parts (22 bits).  So do
+//    their and fp16 inputs' probabilities; bf16 inputs' are rounded to fp16,
 //    2^-12 relative: an eighth of the rounding of a bf16 output.
 //  * What the probabilities refer to follows the scores only where a lane's sum
 //    of a tile passes 2^P_TOP, so no maximum is formed for most tiles.
@@ -679,7 +682,7 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_wide_kernel(PagedAttn a) {
 // they meet in LDS.  What a group needs is asked for before any of it is used.
 template <int DT, int SG>
 __global__ __launch_bounds__(256) void paged_combine_kernel(PagedAttn a) {
-  constexpr int TB = SG == 1 ? 2 : 8;                  // units at a time
+  constexpr int TB = SG == 1 ? 2 : 8;  // units at a time
   constexpr int TN = SG == 1 ? 4 : 8;  // nodes at a time
   __shared__ float4 so[SG > 1 ? 256 : 1];
   __shared__ float2 sml[SG > 1 ? 256 : 1];

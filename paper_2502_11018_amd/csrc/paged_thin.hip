@@ -1,6 +1,7 @@
-// Attention over the 8-bit paged cache (paged.h) for at most 16 rows a KV head
-// (rows: heads of the group x nodes): single tokens and short chains, where
-// reading the cache is the work.
+// Attention over the 8-bit paged cache (paged.h) in row tiles of 16 (rows: heads
+// of the group x nodes): single tokens and short chains, where reading the cache
+// is the work (32 tokens over up to 16384 slots: 605 MB in 110 us, 5.5 TB/s), and
+// calls too short to fill the chip, where its latency is.
 //
 // The same products as in paged_attention.hip with v_mfma_f32_16x16x32: S^T =
 // K Q^T in two groups of 16 keys, O^T += V^T P^T in groups of 16 dims.  MFMA
