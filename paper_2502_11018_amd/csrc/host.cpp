@@ -856,6 +856,7 @@ static int verify_init(const griffin_model_desc* desc, const griffin_weights* w,
     if (window < 0 || sinks < 0) return GRIFFIN_EINVAL;
     if (pool.Hkv != d.n_kv_heads || pool.dh != d.head_dim || d.kv_capacity % pages->page_slots != 0) return GRIFFIN_ESHAPE;
     if (!paged_sizes(pool, d.max_batch, d.max_tree, d.n_q_heads)) return GRIFFIN_ESHAPE;
+    if ((long long)d.max_batch * (d.kv_capacity / pages->page_slots) > (1 << 26)) return GRIFFIN_ESHAPE;  // the table
   }
 
   griffin_ctx* c = new (std::nothrow) griffin_ctx();

@@ -15,7 +15,7 @@ import numpy as np
 import torch
 
 from . import _native as N
-from .paged import _pool_fields, layer_pool, paged_append
+from .paged import _pool_fields, layer_pool, paged_append, paged_read
 
 
 def _i32(a) -> np.ndarray:
@@ -251,7 +251,9 @@ class TreeVerifier:
         self.pages[seq, first:first + len(pages)] = pages
 
     def read_v(self, layer: int, seq: int, n: int) -> torch.Tensor:
-        """Cached values of slots [0, n) as [Hkv, n, dh]."""
+        """Cached values of slots [0, n) as [Hkv, n, dh] (paged: fp32)."""
+        if self.pool is not None:
+            return paged_read(layer_pool(self.pool, layer), torch.from_numpy(self.pages[seq]), n)[1]
         tiles = self._v_tiles(layer, seq)
         Hkv, nt, dh, _ = tiles.shape
         return tiles.transpose(-1, -2).reshape(Hkv, nt * 32, dh)[:, :n]

@@ -195,6 +195,7 @@ def test_loop_commits_what_was_accepted(name, window):
                 n = p.prefix[b]
                 table = torch.from_numpy(p.table[b].astype(np.int32)).cuda()
                 got = [t.double().cpu().numpy() for t in p.G.paged_read(p.G.layer_pool(p.pool, l), table, n)]
+                np.testing.assert_array_equal(p.v.read_v(l, b, n).cpu().numpy(), got[1])
                 for x, y in zip(got, OP.read(p.caches[0][l], p.table[b], n)):
                     # a neighbouring number, at most; few of them
                     assert (np.abs(x - y) <= np.maximum(np.abs(y) / 8, np.abs(y).max() / 448 / 64)).all()
