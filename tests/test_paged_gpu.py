@@ -367,9 +367,14 @@ def on_gpu(pool, table, length, q, k, v, anc, window, sinks):
     (64, 7, 1, 64, [2049, 640], 32, 0),                # several row blocks
     (128, 2, 1, 50, [12000, 100, 700], 32, 3000),
     (64, 4, 1, 61, [12000, 65, 20000], 64, 9000),
+    (128, 4, 2, 45, [700, 8000, 0], 64, 0),            # four waves of 128 dims
+    (128, 4, 2, 20, [5000, 33, 64], 64, 0),            # two row tiles and less: one to a workgroup
+    (64, 3, 1, 17, [31, 2049, 4000], 32, 0),
+    (128, 32, 16, 20, [2500, 100, 5000, 3000], 32, 1800),  # a window
+    (64, 1, 1, 64, [1, 3000, 190], 64, 1000),
 ])
 def test_many_rows(G, dtype, dh, hq, heads, nodes, lengths, page, window):
-    """More than two row tiles a key head, under a launch for long sequences:
+    """More rows a key head than 16, under a launch for long sequences:
     units from one tile to hundreds, full and partial, against fp64 on the GPU."""
     B, used = len(lengths), [-(-n // page) for n in lengths]
     pages = sum(used) + 1
@@ -422,8 +427,10 @@ def test_masks_that_leave_rows_empty(G):
     x = torch.randn(1, 4, 1, 64, device="cuda")
     zero = torch.zeros(1, dtype=torch.int32, device="cuda")
     masks = torch.tensor([[0, 1 << 60, 4, 3]], device="cuda")
-    out = G.paged_attention(pool, torch.zeros(1, 1, dtype=torch.int32, device="cuda"), zero, x, x, x, anc=masks)
-    assert (out[0, :2] == 0).all() and torch.equal(out[0, 2], x[0, 2]) and out.isfinite().all()
+    for cols in (1, 2000):
+        table = torch.zeros(1, cols, dtype=torch.int32, device="cuda")
+        out = G.paged_attention(pool, table, zero, x, x, x, anc=masks)
+        assert (out[0, :2] == 0).all() and torch.equal(out[0, 2], x[0, 2]) and out.isfinite().all()
 
 
 def test_large_and_small_scores(G):
@@ -501,64 +508,75 @@ def test_small_values_beside_large_ones(G, nodes, group, batch, length, dtype, s
     assert ((out - want).abs() <= want * (2.0**-19 + torch.finfo(DT[dtype]).eps / 2) + 3.5 * length * np.exp(-40.0)).all()
 
 
-def test_nan_in_masked_places(G):
+def roomy(table, cols):
+    """The table with entries that name no page behind its own: the launch is
+    planned for what it could hold, which chooses the kernel."""
+    return torch.cat([table, table.new_full((table.shape[0], cols - table.shape[1]), -1)], 1)
+
+
+@pytest.mark.parametrize("nodes,group,cols,batch", [(10, 1, 4, 1), (10, 1, 1000, 1), (10, 1, 4, 300), (40, 1, 4, 1), (40, 1, 1500, 1),
+                                                    (40, 1, 4, 400), (40, 2, 5000, 1), (40, 2, 4, 2800)])
+def test_nan_in_masked_places(G, nodes, group, cols, batch):
     """NaN in slots behind the cached ones, in pages outside the window, and in
     nodes that are not ancestors reaches no row; a NaN inside reaches exactly
     the rows that see it."""
     pool, cache = make_pool(G, 4, 1, 64, 64)
     table = tables(1, 4, 4)
-    n, window, nodes = 200, 50, 40
+    n, window = 200, 50
     fill(G, pool, cache, table, [n], 3, False)
     pages = table[0].tolist()
     clean = [t.clone() for t in pool]
-    lens = torch.tensor([n], dtype=torch.int32, device="cuda")
-    x = torch.randn(3, 1, nodes, 1, 64, device="cuda").to(torch.bfloat16)
-    want = G.paged_attention(pool, table, lens, *x, window=window, sinks=2)
+    lens = torch.full((batch,), n, dtype=torch.int32, device="cuda")
+    table = roomy(table, cols).repeat(batch, 1)  # many sequences that read the same pages
+    q, k, v = torch.randn(1, nodes, group + 2, 64, device="cuda").to(torch.bfloat16).repeat(batch, 1, 1, 1).split([group, 1, 1], 2)
+    want = G.paged_attention(pool, table, lens, q, k, v, window=window, sinks=2)
     # keys and values that no node sees: [2, n - window + 1) and [n, ..)
     for s in list(range(2, n - window + 1)) + list(range(n, 256)):
         pg, at = pages[s // 64], s % 64
         pool.k.view(torch.uint8)[pg, :, at // 32, :, at % 32] = 0x7f
         pool.v.view(torch.uint8)[pg, :, at // 32, :, at % 32] = 0xff
-    got = G.paged_attention(pool, table, lens, *x, window=window, sinks=2)
-    assert torch.equal(got, want)
+    got = G.paged_attention(pool, table, lens, q, k, v, window=window, sinks=2)
+    assert torch.equal(got, want) and (got == got[:1]).all()
     # a slot that the first five nodes see
     s = n - window + 5
     pg, at = pages[s // 64], s % 64
     pool.v.view(torch.uint8)[pg, :, at // 32, 17, at % 32] = 0x7f
-    got = G.paged_attention(pool, table, lens, *x, window=window, sinks=2)
-    assert got[0, :5, 0, 17].isnan().all() and torch.equal(got[0, 5:], want[0, 5:])
-    assert torch.equal(got[0, :5, 0, :17], want[0, :5, 0, :17])
+    got = G.paged_attention(pool, table, lens, q, k, v, window=window, sinks=2)
+    assert got[:, :5, :, 17].isnan().all() and torch.equal(got[:, 5:], want[:, 5:])
+    assert torch.equal(got[:, :5, :, :17], want[:, :5, :, :17])
     # nodes that are not ancestors
     for t, c in zip(pool, clean):
         t.copy_(c)
-    y = x.clone()
-    y[1:, :, 3] = float("nan")
-    anc = torch.tensor([[(1 << (i + 1)) - 1 & ~8 if i != 3 else 15 for i in range(nodes)]], device="cuda")
-    ok = G.paged_attention(pool, table, lens, *x, anc=anc)
-    got = G.paged_attention(pool, table, lens, *y, anc=anc)
-    assert got[0, 3].isnan().all()
+    kn, vn = k.clone(), v.clone()
+    kn[:, 3] = vn[:, 3] = float("nan")
+    anc = torch.tensor([[(1 << (i + 1)) - 1 & ~8 if i != 3 else 15 for i in range(nodes)]], device="cuda").repeat(batch, 1)
+    ok = G.paged_attention(pool, table, lens, q, k, v, anc=anc)
+    got = G.paged_attention(pool, table, lens, q, kn, vn, anc=anc)
+    assert got[:, 3].isnan().all()
     keep = [i for i in range(nodes) if i != 3]
-    assert torch.equal(got[0, keep], ok[0, keep])
+    assert torch.equal(got[:, keep], ok[:, keep])
 
 
-def test_attention_tells_what_is_out_of_range(G):
+@pytest.mark.parametrize("nodes,group,cols", [(2, 1, 3), (2, 1, 400), (20, 1, 3), (20, 1, 1500), (40, 2, 2000)])
+def test_attention_tells_what_is_out_of_range(G, nodes, group, cols):
     """Bad pages and lengths give NaN rows and a status bit, for their
     sequences alone; entries of pages that no node sees are not read."""
     i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
     pool, cache = make_pool(G, 9, 1, 64, 64)
     table = tables(3, 3, 9)
     fill(G, pool, cache, table, [190, 190, 190], 0)
-    x = torch.randn(3, 3, 2, 1, 64, device="cuda")
+    table, past = roomy(table, cols), 64 * cols + 1
+    x = torch.randn(3, nodes, group + 2, 64, device="cuda").split([group, 1, 1], 2)
     want = G.paged_attention(pool, table, i32(190, 190, 190), *x)
     status = i32(0)
-    got = G.paged_attention(pool, table, i32(190, 193, -4), *x, status=status)
+    got = G.paged_attention(pool, table, i32(190, past, -4), *x, status=status)
     assert status.item() == 2 and torch.equal(got[0], want[0]) and got[1:].isnan().all()
     status, bad = i32(0), table.clone()
     bad[1, 1], bad[2, 2] = 9, -1
     got = G.paged_attention(pool, bad, i32(190, 190, 190), *x, status=status)
     assert status.item() == 1 and torch.equal(got[0], want[0]) and got[1:].isnan().all()
     status = i32(0)
-    got = G.paged_attention(pool, table, i32(190, 190, 190), *x, counts=i32(2, 3, -1), status=status)
+    got = G.paged_attention(pool, table, i32(190, 190, 190), *x, counts=i32(nodes, nodes + 1, -1), status=status)
     assert status.item() == 2 and torch.equal(got[0], want[0]) and got[1].isnan().all()
     want = G.paged_attention(pool, table, i32(190, 190, 190), *x, window=20)
     bad = table.clone()
@@ -568,25 +586,27 @@ def test_attention_tells_what_is_out_of_range(G):
     assert status.item() == 0
 
 
-def test_attention_takes_any_strides(G):
+@pytest.mark.parametrize("nodes,cols", [(5, 2), (5, 3000), (25, 2), (25, 3000), (64, 5000)])
+def test_attention_takes_any_strides(G, nodes, cols):
     pool, cache = make_pool(G, 4, 2, 64, 64)
     table = tables(2, 2, 4)
     fill(G, pool, cache, table, [100, 65], 0)
+    table = roomy(table, cols)
     lens = torch.tensor([100, 65], dtype=torch.int32, device="cuda")
     for dt in (torch.bfloat16, torch.float32):
-        raw = torch.randn(1 + 2 * 5 * (8 * 64 + 7), device="cuda").to(dt)
-        x = raw[1:].view(2, 5, 8 * 64 + 7)[:, :, 5:5 + 8 * 64].unflatten(2, (8, 64))
+        raw = torch.randn(1 + 2 * nodes * (8 * 64 + 7), device="cuda").to(dt)
+        x = raw[1:].view(2, nodes, 8 * 64 + 7)[:, :, 5:5 + 8 * 64].unflatten(2, (8, 64))
         q, k, v = x[:, :, :4], x[:, :, 4:6], x[:, :, 6:]
         want = G.paged_attention(pool, table, lens, q.contiguous(), k.contiguous(), v.contiguous())
         assert torch.equal(G.paged_attention(pool, table, lens, q, k, v), want)
-        wide = torch.full((2, 4, 5, 65), 7.0, dtype=dt, device="cuda")
+        wide = torch.full((2, 4, nodes, 65), 7.0, dtype=dt, device="cuda")
         out = wide[..., 1:].transpose(1, 2)
         assert torch.equal(G.paged_attention(pool, table, lens, q, k, v, out=out), want) and (wide[..., 0] == 7).all()
-        two = torch.stack([table, table], 1).flatten(1)[:, :2]  # a table with a row stride of its own
+        two = torch.stack([table, table], 1).flatten(1)[:, :cols]  # a table with a row stride of its own
         assert torch.equal(G.paged_attention(pool, two, lens, q, k, v), want)
     # heads that share one key head's rows, and a broadcast query
-    q = torch.randn(1, 1, 1, 64, device="cuda").expand(2, 5, 4, 64)
-    k = torch.randn(2, 5, 1, 64, device="cuda").expand(2, 5, 2, 64)
+    q = torch.randn(1, 1, 1, 64, device="cuda").expand(2, nodes, 4, 64)
+    k = torch.randn(2, nodes, 1, 64, device="cuda").expand(2, nodes, 2, 64)
     want = G.paged_attention(pool, table, lens, q.contiguous(), k.contiguous(), k.contiguous())
     assert torch.equal(G.paged_attention(pool, table, lens, q, k, k), want)
 
