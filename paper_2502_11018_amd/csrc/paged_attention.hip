@@ -735,13 +735,13 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(PagedAttn a) {
       for (int x = 0; x < TB; ++x)
         if (s + x * SG < units && !(ml[x].x == NO_MAX && ml[x].y == 0.f)) mn = fmaxf(mn, ml[x].x);
       if (mn == -INFINITY) continue;  // no slot of them is seen
-      const float al = exp2f(m - mn);
+      const float al = __builtin_amdgcn_exp2f(m - mn);
       l *= al;
       o.x *= al, o.y *= al, o.z *= al, o.w *= al;
 #pragma unroll
       for (int x = 0; x < TB; ++x)
         if (s + x * SG < units) {
-          const float e = exp2f(ml[x].x - mn);
+          const float e = __builtin_amdgcn_exp2f(ml[x].x - mn);
           l += e * ml[x].y;
           o.x += e * ou[x].x, o.y += e * ou[x].y, o.z += e * ou[x].z, o.w += e * ou[x].w;
         }
@@ -756,14 +756,14 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(PagedAttn a) {
         float mn = m;
 #pragma unroll
         for (int g = 1; g < SG; ++g) mn = fmaxf(mn, sml[g * (256 / SG) + t].x);
-        const float al = m == -INFINITY ? 0.f : exp2f(m - mn);
+        const float al = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
         l *= al;
         o.x *= al, o.y *= al, o.z *= al, o.w *= al;
 #pragma unroll
         for (int g = 1; g < SG; ++g) {
           const float2 x = sml[g * (256 / SG) + t];
           const float4 v = so[g * (256 / SG) + t];
-          const float e = x.x == -INFINITY ? 0.f : exp2f(x.x - mn);
+          const float e = x.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x.x - mn);
           l += e * x.y;
           o.x += e * v.x, o.y += e * v.y, o.z += e * v.z, o.w += e * v.w;
         }
@@ -785,15 +785,16 @@ int paged_plan(PagedAttn& a, int max_length) {
   if (a.cut.window)
     most = std::min(most, ((long long)a.cut.window + 30) / 32 + 1 + ((long long)a.cut.sinks + 31) / 32);
   if (most * a.batch > 0x7fffffffLL) return -1;
-  // The wide kernel where a KV head has more than two row tiles and its units
-  // are long: at least 32 tiles for each of the 256 workgroups that then fill
-  // the chip.
+  // The wide kernel where a KV head has more than two row tiles and either half
+  // of the CUs get a whole sequence each (32 x 61 nodes of 4 x 8 heads over 512
+  // slots: 36 us against 58, 8 of them 24 against 22), or its units are long: at
+  // least 32 tiles for each of the 256 workgroups that then fill the chip.
   const int nw = R > 128 ? 8 : 4, wide_blocks = (R + 32 * nw - 1) / (32 * nw), thin_blocks = (R + 15) / 16;
-  a.wide = R > 64 && a.batch * most * a.pool.Hkv * wide_blocks >= 32 * 256 ? nw : 0;
+  const long long whole = (long long)a.batch * a.pool.Hkv * wide_blocks;
+  a.wide = R > 64 && (whole >= 128 || most * whole >= 32 * 256) ? nw : 0;
   // Row tiles of 16 where one holds all rows, and where all workgroups fit the
   // chip at once, as a wave then has half of the work: 61 nodes of 4 heads over
-  // 500 slots 8 us against 10 (512 workgroups), over 2048 slots 13 against 12
-  // (1152), of 1 head in fp32 over 1024 slots 17 against 20 (512).
+  // 500 slots 8 us against 10 (256 workgroups), over 2077 13 against 12 (1152).
   const long long by_len = (long long)a.batch * ((most + UNIT_LEAST - 1) / UNIT_LEAST);
   a.thin = R <= 16 || by_len * a.pool.Hkv * thin_blocks <= 1024;
   // One workgroup of eight waves for all of a (sequence, KV head), which reads
