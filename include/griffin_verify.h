@@ -515,8 +515,8 @@ typedef struct griffin_attention {
  * 2^-33 of the row's largest at least.  The rows of a
  * sequence with an invalid page or length become NaN.  Head h reads KV head
  * h / (n_q_heads / n_kv_heads).  The workspace (16-byte aligned, of
- * griffin_paged_attention_workspace bytes; 0 for arguments that the call
- * refuses) belongs to the call until its work is done.  The same call gives the same
+ * griffin_paged_attention_workspace bytes; 0: none, and for arguments that the
+ * call refuses) belongs to the call until its work is done.  The same call gives the same
  * bits; the other sequences' lengths can change a sequence's last bits.
  * Errors: EINVAL, ESHAPE, ETREE (nodes), ECAPACITY (max_length beyond the
  * table), ENOMEM (workspace_bytes), EHIP. */

@@ -4,7 +4,6 @@
 
 #include <hip/hip_runtime.h>
 
-#include <algorithm>
 #include <cmath>
 
 #include "griffin_verify.h"
@@ -131,7 +130,7 @@ int griffin_paged_append(const griffin_append* g, void* hip_stream) {
 size_t griffin_paged_attention_workspace(const griffin_attention* g) {
   PagedAttn a;
   if (!g || attention_args(g, &a) != GRIFFIN_OK) return 0;
-  return std::max<size_t>(paged_workspace(a, nullptr), 256);
+  return paged_workspace(a, nullptr);
 }
 
 int griffin_paged_attention(const griffin_attention* g, void* workspace, size_t workspace_bytes, void* hip_stream) {

@@ -129,7 +129,7 @@ def _on(stream, call, pool, *tensors, **named):
 
 def _call(fn, dev, *args):
     """A library call with the device's current stream as its last argument."""
-    if torch.cuda.current_device() != dev.index:
+    if torch._C._cuda_getDevice() != dev.index:
         with torch.cuda.device(dev):
             rc = fn(*args, torch._C._cuda_getCurrentRawStream(dev.index))
     else:
@@ -213,6 +213,9 @@ def paged_attention(pool: Sequence[torch.Tensor], table: torch.Tensor, lengths: 
                       *_rows(out, "out", dev, dtype, shape), dh ** -0.5 if scale is None else scale, stride, cols,
                       -1 if max_length is None else max_length, b, nodes, hq, _DTYPES[dtype], window, sinks)
     need = N.lib.griffin_paged_attention_workspace(args)
-    work = torch.empty(need, dtype=torch.uint8, device=dev)
-    _call(N.lib.griffin_paged_attention, dev, args, work.data_ptr(), need)
+    if need:
+        work = torch.empty(need, dtype=torch.uint8, device=dev)
+        _call(N.lib.griffin_paged_attention, dev, args, work.data_ptr(), need)
+    else:
+        _call(N.lib.griffin_paged_attention, dev, args, None, 0)
     return out

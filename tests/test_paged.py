@@ -131,6 +131,7 @@ def test_attention_refuses(code, kw):
 
 def test_attention_wants_its_workspace():
     N = _lib()
+    assert N.lib.griffin_paged_attention_workspace(attention_args(most=100)) == 0  # whole sequences: none
     # 5 nodes of 4 heads on each of 2 key heads: 20 rows, which units share
     args = attention_args(most=100, nodes=5, hq=8)
     need = N.lib.griffin_paged_attention_workspace(args)
