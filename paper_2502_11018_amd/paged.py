@@ -66,18 +66,18 @@ def paged_read(pool: Sequence[torch.Tensor], table: torch.Tensor, n: int):
 
 
 def _pool_fields(pool):
-    """Pointers and sizes of a pool; (fields, heads, head_dim, device)."""
+    """Pointers and sizes of a pool; (fields, heads, head_dim, device's index)."""
     k, v, ke, ve = pool
-    ks, dev = k.shape, k.device
-    if len(ks) != 6 or ks[4:] != (32, 16) or k.dtype is not _E4M3 or v.dtype is not _E4M3 or \
-            ke.dtype is not torch.int8 or ve.dtype is not torch.int8:
+    if k.dim() != 6 or k.dtype is not _E4M3 or v.dtype is not _E4M3 or ke.dtype is not torch.int8 or \
+            ve.dtype is not torch.int8:
         raise ValueError("a pool is (k, v, k_exp, v_exp) as paged_pool lays them out")
-    n, heads, tpp, chunks = ks[:4]
-    dh = chunks * 16
-    if v.shape != (n, heads, tpp, dh, 32) or ke.shape != ks[:3] or ve.shape != ks[:3] or not (
+    n, heads, tpp, chunks, slots, dims = k.shape
+    dh, tiles = chunks * 16, (n, heads, tpp)
+    if slots != 32 or dims != 16 or v.shape != (n, heads, tpp, dh, 32) or ke.shape != tiles or ve.shape != tiles or not (
             k.is_contiguous() and v.is_contiguous() and ke.is_contiguous() and ve.is_contiguous()):
         raise ValueError("a pool's tensors must be contiguous and of the same pages, heads and head_dim")
-    if dev.type != "cuda" or v.device != dev or ke.device != dev or ve.device != dev:
+    dev = k.get_device()
+    if dev < 0 or v.get_device() != dev or ke.get_device() != dev or ve.get_device() != dev:
         raise ValueError("a pool lies on one CUDA device")
     return (k.data_ptr(), v.data_ptr(), ke.data_ptr(), ve.data_ptr(), n, tpp * 32, heads, dh), heads, dh, dev
 
@@ -86,27 +86,30 @@ def _ints(t: Optional[torch.Tensor], what: str, dev, shape, dtype=torch.int32) -
     """Address of an optional contiguous integer tensor."""
     if t is None:
         return 0
-    if t.dtype is not dtype or t.shape != shape or t.device != dev or not t.is_contiguous():
-        raise ValueError(f"{what} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {dev}")
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous {dtype} tensor of shape {tuple(shape)} on cuda:{dev}")
     return t.data_ptr()
 
 
 def _table(table: torch.Tensor, lengths: torch.Tensor, dev):
-    if table.dtype is not torch.int32 or table.dim() != 2 or table.device != dev or table.stride(1) != 1:
-        raise ValueError(f"table must be an int32 [batch, pages] tensor on {dev}")
+    if table.dtype is not torch.int32 or table.dim() != 2 or table.get_device() != dev:
+        raise ValueError(f"table must be an int32 [batch, pages] tensor on cuda:{dev}")
     b, cols = table.shape
+    stride, unit = table.stride()
+    if unit != 1:
+        raise ValueError("table: a sequence's pages must be contiguous")
     # the stride of a single row is not used (and may be anything)
-    return b, cols, table.stride(0) if b > 1 else cols, _ints(lengths, "lengths", dev, (b,))
+    return b, cols, stride if b > 1 else cols, _ints(lengths, "lengths", dev, (b,))
 
 
 def _rows(t: torch.Tensor, what: str, dev, dtype, shape):
     """Address and strides of rows [batch, rows, heads, dh]."""
-    if t.dtype is not dtype or t.shape != shape or t.device != dev:
-        raise ValueError(f"{what} must be a {dtype} tensor of shape {tuple(shape)} on {dev}")
-    s = t.stride()
-    if s[3] != 1:
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev:
+        raise ValueError(f"{what} must be a {dtype} tensor of shape {tuple(shape)} on cuda:{dev}")
+    seq, row, head, unit = t.stride()
+    if unit != 1:
         raise ValueError(f"{what}: the last dimension must be contiguous")
-    return t.data_ptr(), s[0], s[1], s[2]
+    return t.data_ptr(), seq, row, head
 
 
 def _on(stream, call, pool, *tensors, **named):
@@ -129,11 +132,11 @@ def _on(stream, call, pool, *tensors, **named):
 
 def _call(fn, dev, *args):
     """A library call with the device's current stream as its last argument."""
-    if torch._C._cuda_getDevice() != dev.index:
+    if torch._C._cuda_getDevice() != dev:
         with torch.cuda.device(dev):
-            rc = fn(*args, torch._C._cuda_getCurrentRawStream(dev.index))
+            rc = fn(*args, torch._C._cuda_getCurrentRawStream(dev))
     else:
-        rc = fn(*args, torch._C._cuda_getCurrentRawStream(dev.index))
+        rc = fn(*args, torch._C._cuda_getCurrentRawStream(dev))
     if rc != N.GRIFFIN_OK:
         raise N.GriffinError(rc, fn.__name__)
 

@@ -177,7 +177,7 @@ class TreeVerifier:
             if k_cache is not None or v_cache is not None:
                 raise ValueError("a cache is k_cache and v_cache, or a pool")
             fields, heads, pool_dh, pool_dev = _pool_fields(layer_pool(pool, 0))
-            if any(t.dim() < 4 or t.shape[0] != L or not t.is_contiguous() for t in pool) or pool_dev != dev:
+            if any(t.dim() < 4 or t.shape[0] != L or not t.is_contiguous() for t in pool) or pool_dev != weights.embed.get_device():
                 raise ValueError(f"the pool's tensors must be contiguous with {L} layers on {dev}")
             page = fields[5]
             if kv_capacity % page:
