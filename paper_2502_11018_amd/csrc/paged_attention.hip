@@ -678,12 +678,12 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_wide_kernel(PagedAttn a) {
 
 // Joins a row's units and the nodes of its own root path: a thread holds 4 dims
 // of a head of one node.  SG groups of threads share a head where there are few
-// rows: group g takes units g, g + SG, .., the last one the root path too, and
-// they meet in LDS.  What a group needs is asked for before any of it is used.
+// rows: group g takes units and nodes g, g + SG, .., and they meet in LDS.  What
+// a group needs is asked for before any of it is used.
 template <int DT, int SG>
 __global__ __launch_bounds__(256) void paged_combine_kernel(PagedAttn a) {
   constexpr int TB = SG == 1 ? 2 : 8;  // units at a time
-  constexpr int TN = SG == 1 ? 4 : 8;  // nodes at a time
+  constexpr int TN = 4;                // nodes at a time
   __shared__ float4 so[SG > 1 ? 256 : 1];
   __shared__ float2 sml[SG > 1 ? 256 : 1];
   const int dh = a.pool.dh, quads = dh / 4, heads = 256 / SG / quads;  // heads of a workgroup
@@ -727,7 +727,7 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(PagedAttn a) {
     };
     RootPath<DT, TN> path;
     ask(grp);
-    path.start(a, b, hk, d, grp == SG - 1 ? anc : 0, depth_of(anc, i), len);
+    path.start(a, b, hk, d, anc, SG == 1 ? ~0ull : 0x1111111111111111ull << grp, depth_of(anc, i), len);
     for (int s = grp; s < units; s += TB * SG) {
       if (s != grp) ask(s);
       float mn = m;
@@ -854,8 +854,13 @@ hipError_t launch_paged_attention(const PagedAttn& a, hipStream_t s) {
     if (a.pool.dh == 128) launch_form<128>(a, dim3((unsigned)wgs), s);
     else launch_form<64>(a, dim3((unsigned)wgs), s);
   }
-  // four groups a head while that leaves at most two workgroups for each CU
-  const bool few = (long long)a.batch * a.nodes * a.Hq * (a.pool.dh / 4) <= 512 * 64;
+  // Four groups a head while that leaves at most four workgroups for each CU (a
+  // chain of 61 nodes of 32 heads 10 us against 16, 40 nodes of a tree 5.3 against
+  // 6.0; 4 chains 27 against 24), of fp32 trees, whose groups take more registers,
+  // two (61 nodes 7.9 against 5.6; a chain's long paths gain all the same: 12.5
+  // against 17.8).
+  const int most = a.dtype == PT_F32 && a.anc ? 512 : 1024;
+  const bool few = (long long)a.batch * a.stride * a.Hq * (a.pool.dh / 4) <= most * 64;
   if (a.dtype == PT_F32) launch_combine<PT_F32>(a, few, s);
   else if (a.dtype == PT_F16) launch_combine<PT_F16>(a, few, s);
   else launch_combine<PT_BF16>(a, few, s);

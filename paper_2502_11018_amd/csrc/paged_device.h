@@ -348,34 +348,36 @@ __device__ __forceinline__ float xor16(float x) {
 template <int DT, int TN>
 struct RootPath {
   typename QuadOf<DT>::type k4[TN], v4[TN];
-  uint64_t anc;
+  uint64_t path, anc;  // all of the path; what is left of this thread's part of it
   long long kb, vb;
-  int dep, len, r, seen;
+  int dep, len, seen;
+  bool any;
 
   __device__ __forceinline__ void ask(const PagedAttn& a) {
     seen = 0;
 #pragma unroll
     for (int x = 0; x < TN; ++x) {
       if (!anc) break;  // uniform
-      const int j = __builtin_ctzll(anc);
+      const int j = __builtin_ctzll(anc), r = __builtin_popcountll(path & ((1ull << j) - 1));
       anc &= anc - 1;
       if (!a.cut.window || dep - r < a.cut.window || (long long)len + r < a.cut.sinks) seen |= 1 << x;
-      ++r;
       k4[x] = load_quad<DT>(a.k.p, kb + j * a.k.sr, a.k.vec);
       v4[x] = load_quad<DT>(a.v.p, vb + j * a.v.sr, a.v.vec);
     }
   }
-  __device__ __forceinline__ void start(const PagedAttn& a, int b, int hk, int d, uint64_t nodes, int depth, int length) {
-    anc = nodes;
+  // part: the bits of the path that are this thread's
+  __device__ __forceinline__ void start(const PagedAttn& a, int b, int hk, int d, uint64_t nodes, uint64_t part, int depth, int length) {
+    path = nodes;
+    anc = nodes & part;
+    any = anc != 0;
     dep = depth;
     len = length;
     kb = b * a.k.sb + hk * a.k.sh + d;
     vb = b * a.v.sb + hk * a.v.sh + d;
-    r = 0;
     ask(a);
   }
   __device__ __forceinline__ void add(const PagedAttn& a, const float4& q, int quads, float& m, float& l, float4& o) {
-    for (bool any = r > 0; any;) {
+    while (any) {
       if (seen) {
         float sc[TN];
 #pragma unroll

@@ -217,7 +217,7 @@ __device__ __forceinline__ void write_rows(const PagedAttn& a, const Place& p, i
     const uint64_t anc = anc_of(a, p.b, node);
     const float4 q = query_quad<DT>(a, p.b * a.q.sb + node * a.q.sr + h * a.q.sh + d);
     RootPath<DT, 4> path;
-    path.start(a, p.b, p.hk, d, anc, depth_of(anc, node), p.sight.len);
+    path.start(a, p.b, p.hk, d, anc, ~0ull, depth_of(anc, node), p.sight.len);
     float m, l;
     float4 o;
     join(r, c, m, l, o);
